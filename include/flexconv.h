@@ -406,6 +406,106 @@ int flexupsample_bwd(const float *grad_out, const int32_t *argmax, const int32_t
 int flex_validate_selection(const int32_t *sel, int B, int Ns, int Nf, int32_t *bad_count_dev,
                             void *workspace, size_t workspace_bytes, void *stream);
 
+/*
+ * The operators around a network's layers: layer norm, log probabilities of classes or tokens, optimizer step.
+ * Their tensors are fp32, bf16 or fp16 (a flex_dtype), [B,C,N] or [B,N,C] by the layout flag; what they compute is computed in
+ * fp32, and rounded once, to nearest, where it is stored.  Statistics, log probabilities and their gradients are fp32.
+ * Any alignment of an element's size is taken.
+ */
+typedef enum { FLEX_F32 = 0, FLEX_BF16 = 1, FLEX_F16 = 2 } flex_dtype;
+
+/*
+ * Layer norm over the C channels of every position:
+ *   y = (x - mean) * rstd * weight + bias,  mean over the channels,  rstd = 1 / sqrt(mean((x - mean)^2) + eps)
+ * weight / bias [C] in param_dtype (FLEX_F32 or x's type); both NULL: not scaled.  mean / rstd fp32 [B,N] for the backward pass;
+ * either may be NULL.  y must not overlap x (y == x is refused).  eps >= 0.
+ */
+int flexnorm_fwd(const void *x, const void *weight, const void *bias, void *y, float *mean, float *rstd,
+                 int B, int N, int C, float eps, int dtype, int param_dtype, int layout, void *stream);
+
+/*
+ * Layer norm backward, from mean / rstd of the forward pass; with xh = (x - mean) rstd, h = grad_out weight:
+ *   grad_x = rstd (h - mean(h) - xh mean(h xh)),  grad_weight = sum of grad_out xh,  grad_bias = sum of grad_out over all positions
+ * grad_x in x's type, or NULL, over neither x nor grad_out; grad_weight / grad_bias [C] in param_dtype, both or neither NULL.  weight NULL: taken as ones.
+ * No atomics: the sums over positions are added in a fixed order (partial sums in the workspace), so results are reproducible.
+ * The workspace is needed with grad_weight only.
+ */
+size_t flexnorm_bwd_workspace_bytes(int B, int N, int C, int dtype, int layout);
+int flexnorm_bwd(const void *x, const void *weight, const void *grad_out, const float *mean, const float *rstd,
+                 void *grad_x, void *grad_weight, void *grad_bias, int B, int N, int C, int dtype, int param_dtype,
+                 int layout, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Log probabilities over the C scores of every position (classes of a point, tokens of a vocabulary):
+ *   lse = ln sum_c exp(x_c),  logp = x_target - lse,  entropy = - sum_c p_c ln p_c,  p_c = exp(x_c - lse)
+ * and the `top` (0 .. FLEX_LOGP_MAX_TOP, at most C) largest log probabilities, in descending order, with their classes; equal
+ * scores: the lower class first.
+ * target int32 [B,N], or NULL (then logp too); a target outside [0,C), -1 say, marks a position to be ignored: its scores are not
+ * looked at, logp = entropy = lse = 0, no alternatives.  logp, entropy, lse fp32 [B,N]; top_logp fp32 and top_class int32
+ * [B,N,top] point-major, [B,top,N] channel-major (not touched if top = 0).
+ * A score of -inf is a masked class: no share, never an alternative; where fewer classes are left than asked for, the others are
+ * (-inf, -1).  A position with nothing but -inf has lse = logp = -inf, entropy 0.  NaN or +inf among the scores: logp, entropy and
+ * lse are NaN, NaN is never an alternative.
+ * row_stride (elements): point-major from one position's scores to the next one's, at least C (rows of a padded vocabulary);
+ * channel-major from one class's scores to the next one's, at least N.  C <= FLEX_LOGP_MAX_CLASSES.
+ */
+#define FLEX_LOGP_MAX_CLASSES (1 << 20)
+#define FLEX_LOGP_MAX_TOP 32
+size_t flexlogp_fwd_workspace_bytes(int B, int N, int C, int top, int dtype, int layout);
+int flexlogp_fwd(const void *logits, const int32_t *target, float *logp, float *entropy, float *lse,
+                 float *top_logp, int32_t *top_class, int B, int N, int C, int top, int64_t row_stride, int dtype,
+                 int layout, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Gradient of the scores from those of logp and of entropy (either may be NULL; grad_logp needs target, grad_entropy needs entropy),
+ * lse and entropy as the forward pass left them:
+ *   grad_x_c = grad_logp ([c = target] - p_c) - grad_entropy p_c (x_c - lse + entropy)
+ * Zero at ignored positions (whatever their scores and gradients) and at those with lse = -inf.  A cross entropy's mean over n
+ * positions is grad_logp = -1 / n.  grad_logits in the scores' type with rows of its own stride; it may be the scores' own memory
+ * if the strides agree.  The elements between two rows are left as they are.
+ */
+int flexlogp_bwd(const void *logits, const int32_t *target, const float *lse, const float *entropy,
+                 const float *grad_logp, const float *grad_entropy, void *grad_logits, int B, int N, int C,
+                 int64_t row_stride, int64_t grad_row_stride, int dtype, int layout, void *stream);
+
+/*
+ * AdamW over a list of tensors in one call (Sec. 5: the paper trains with Adam), t = number of the step, g = gradient * grad_scale:
+ *   m = beta1 m + (1 - beta1) g,  v = beta2 v + (1 - beta2) g^2
+ *   p = p (1 - lr weight_decay) - lr (m / (1 - beta1^t)) / (sqrt(v / (1 - beta2^t)) + eps)
+ * flexadamw_plan_build enters the tensors in device memory of the caller (plan: flexadamw_plan_bytes, 256-byte aligned), which also
+ * holds the step's number, so that a captured step counts on in every replay; it fills *out, a handle of plain values for
+ * flexadamw_step.  The plan is valid as long as the tensors stay where they are; calls that share one must be stream-ordered.
+ * `steps`: how many steps were done before (0 for a new run; the int64 at FLEX_ADAMW_STEPS_AT bytes of the plan is the count).
+ *   tensors   host array of n (n <= 2^20); count < 2^31 elements, 0 allowed; no memory twice in the list
+ *   state_bits 32: exp_avg, exp_avg_sq fp32 [count].  8: e4m3 (OCP) bytes [count] and a power of two (e8m0 byte) for every 32 of
+ *             them, [ceil(count / 32)]; exp_avg_sq holds roots: v = (value * scale)^2.  A state is rounded up or down at random so
+ *             that its mean is exact (v in the square), by bits that depend on (seed, step, tensor, element) alone; a v above
+ *             zero is never stored as zero.  All zero bytes are the state before the first step.
+ *   copy      copy_dtype (FLEX_BF16 / FLEX_F16), or NULL: the new values once more, for a network that computes in 16 bits
+ * flexadamw_step: grads host array of n device pointers, all of grad_dtype; NULL: that tensor is left as it is.  lr, or *lr_dev
+ * where lr_dev (device) is not NULL; grad_scale device, or NULL for 1.  A grad_scale that is not finite: nothing is changed and
+ * the step is not counted (a loss scale that overflowed, decided on the device).  Gradients must be finite otherwise.
+ */
+#define FLEX_ADAMW_STEPS_AT 32
+typedef struct {
+    void *param, *exp_avg, *exp_avg_sq;
+    uint8_t *avg_scale, *avg_sq_scale;
+    void *copy;
+    int64_t count;
+    double weight_decay;
+} flex_adamw_tensor;
+typedef struct {
+    void *plan;
+    int64_t chunks;
+    int32_t tensors, param_dtype, state_bits, copy_dtype;
+} flex_adamw;
+size_t flexadamw_plan_bytes(const flex_adamw_tensor *tensors, int n);
+int flexadamw_plan_build(const flex_adamw_tensor *tensors, int n, int param_dtype, int state_bits, int copy_dtype,
+                         double beta1, double beta2, double eps, int64_t steps, uint32_t seed, void *plan,
+                         size_t plan_bytes, flex_adamw *out, void *stream);
+int flexadamw_step(const flex_adamw *adamw, const void *const *grads, int n, int grad_dtype, double lr,
+                   const float *lr_dev, const float *grad_scale, void *stream);
+
 /* Bytes of workspace needed by op (a flex_op) at these sizes. 0 on bad sizes. */
 size_t flexconv_workspace_bytes(int op, int B, int N, int K, int Din, int Dout, int layout);
 /* Bytes of workspace with which op runs fastest: at least flexconv_workspace_bytes.  The convolution's forward and

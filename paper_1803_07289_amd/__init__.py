@@ -14,6 +14,9 @@ import threading
 
 import torch
 
+# element types of the operators around the layers (flexnorm_*, flexlogp_*, flexadamw_*)
+_DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+LOGP_MAX_TOP = 32
 BCN = 0   # [B,C,N]  channel-major, the paper's form
 BNC = 1   # [B,N,C]  point-major, the library's native form
 OP_CONV_FWD, OP_CONV_BWD, OP_CONV_BWD_BUILD, OP_INEDGES, OP_UPSAMPLE = 0, 1, 2, 3, 4
@@ -59,6 +62,15 @@ _SIGS = {
     "flexconv_has_fast_path": (_i, [_i, _i]),
     "flexconv_kernel_route": (_i, [_i] * 7),
     "flex_status_string": (ctypes.c_char_p, [_i]),
+    "flexnorm_fwd": (_i, [_vp] * 6 + [_i] * 3 + [ctypes.c_float] + [_i] * 3 + [_vp]),
+    "flexnorm_bwd_workspace_bytes": (_sz, [_i] * 5),
+    "flexnorm_bwd": (_i, [_vp] * 8 + [_i] * 6 + [_vp, _sz, _vp]),
+    "flexlogp_fwd_workspace_bytes": (_sz, [_i] * 6),
+    "flexlogp_fwd": (_i, [_vp] * 7 + [_i] * 4 + [ctypes.c_int64] + [_i] * 2 + [_vp, _sz, _vp]),
+    "flexlogp_bwd": (_i, [_vp] * 7 + [_i] * 3 + [ctypes.c_int64] * 2 + [_i] * 2 + [_vp]),
+    "flexadamw_plan_bytes": (_sz, [_vp, _i]),
+    "flexadamw_plan_build": (_i, [_vp] + [_i] * 4 + [ctypes.c_double] * 3 + [ctypes.c_int64, ctypes.c_uint32, _vp, _sz, _vp, _vp]),
+    "flexadamw_step": (_i, [_vp, _vp, _i, _i, ctypes.c_double, _vp, _vp, _vp]),
     "flex_calibrate_copy": (_i, [_vp, _vp, _sz, _vp]),
     "flex_calibrate_mfma_f16": (_i, [_i, _vp, ctypes.POINTER(ctypes.c_double), _vp]),
 }
@@ -639,6 +651,289 @@ def flex_validate_neighbors(nbr):
     bad = torch.zeros(1, dtype=torch.int32, device=nbr.device)
     _check(lib().flex_validate_neighbors(_ptr(nbr), B, N, K, _ptr(bad), _stream()), "flex_validate_neighbors")
     return int(bad.item())
+
+
+# ---- the operators around the layers: layer norm, log probabilities, optimizer step -------------------------------------
+
+def _any(t, name, dtypes=_DTYPES):
+    """_dev for a tensor of one of the types `dtypes`, on the current device."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise TypeError(f"{name} must be a CUDA tensor")
+    if t.dtype not in dtypes:
+        raise TypeError(f"{name} must be one of {', '.join(str(d) for d in dtypes)}, got {t.dtype}")
+    if t.device.index != torch.cuda.current_device():
+        raise ValueError(f"{name} is on {t.device}, the current device is cuda:{torch.cuda.current_device()}")
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+    return t
+
+
+_F32 = (torch.float32,)
+
+
+def _norm_args(x, weight, layout):
+    _any(x, "x")
+    if x.dim() != 3:
+        raise ValueError("x must be 3-D")
+    B, N, C = (x.shape[0], x.shape[2], x.shape[1]) if layout == BCN else x.shape
+    if weight is not None and tuple(_any(weight, "weight", (torch.float32, x.dtype)).shape) != (C,):
+        raise ValueError("weight must be [C]")
+    return B, N, C
+
+
+def flexnorm_fwd(x, weight=None, bias=None, eps=1e-5, layout=BCN, out=None):
+    """Layer norm over the channels of every position of x (fp32, bf16 or fp16); weight and bias [C] in fp32 or x's type, both or
+    neither.  Returns (y, mean, rstd), the latter two fp32 [B,N]."""
+    layout = _layout(layout)
+    B, N, C = _norm_args(x, weight, layout)
+    if (weight is None) != (bias is None):
+        raise ValueError("weight and bias: both or neither")
+    if bias is not None and (_any(bias, "bias").dtype != weight.dtype or bias.shape != weight.shape):
+        raise ValueError("bias must be like weight")
+    if out is None:
+        out = torch.empty_like(x)
+    elif _any(out, "out", (x.dtype,)).shape != x.shape:
+        raise ValueError("out has the wrong shape")
+    stats = torch.empty((2, B, N), dtype=torch.float32, device=x.device)
+    mean, rstd = stats.unbind(0)
+    _check(lib().flexnorm_fwd(_ptr(x), _ptr(weight), _ptr(bias), _ptr(out), _ptr(mean), _ptr(rstd), B, N, C, eps, _DTYPES[x.dtype],
+                              0 if weight is None else _DTYPES[weight.dtype], layout, _stream()), "flexnorm_fwd")
+    return out, mean, rstd
+
+
+def flexnorm_bwd(x, weight, grad_out, mean, rstd, layout=BCN, need_x=True, need_params=True, workspace=None):
+    """Layer norm backward.  Returns (grad_x, grad_weight, grad_bias); entries not asked for are None, and so are the parameters'
+    where weight is None."""
+    layout = _layout(layout)
+    B, N, C = _norm_args(x, weight, layout)
+    need_params = need_params and weight is not None
+    if not need_x and not need_params:
+        return None, None, None
+    if _any(grad_out, "grad_out", (x.dtype,)).shape != x.shape:
+        raise ValueError("grad_out must be shaped like x")
+    for t, name in ((mean, "mean"), (rstd, "rstd")):
+        if tuple(_any(t, name, _F32).shape) != (B, N):
+            raise ValueError(f"{name} must be [B,N]")
+    gx = torch.empty_like(x) if need_x else None
+    gw = gb = ws = None
+    ws_bytes = 0
+    if need_params:
+        gw, gb = torch.empty_like(weight), torch.empty_like(weight)
+        ws, ws_bytes = _ws_arg(workspace, x.device, lib().flexnorm_bwd_workspace_bytes(B, N, C, _DTYPES[x.dtype], layout))
+    _check(lib().flexnorm_bwd(_ptr(x), _ptr(weight), _ptr(grad_out), _ptr(mean), _ptr(rstd), _ptr(gx), _ptr(gw), _ptr(gb), B, N, C,
+                              _DTYPES[x.dtype], 0 if weight is None else _DTYPES[weight.dtype], layout, _ptr(ws), ws_bytes,
+                              _stream()), "flexnorm_bwd")
+    return gx, gw, gb
+
+
+def _score_dims(t, layout, name):
+    """(B, N, C, row stride) of class scores: contiguous, or rows (point-major: a position's; channel-major: a class's) that lie
+    evenly spaced, as in a padded vocabulary's first C columns."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise TypeError(f"{name} must be a CUDA tensor")
+    if t.dtype not in _DTYPES:
+        raise TypeError(f"{name} must be fp32, bf16 or fp16, got {t.dtype}")
+    if t.device.index != torch.cuda.current_device():
+        raise ValueError(f"{name} is on {t.device}, the current device is cuda:{torch.cuda.current_device()}")
+    if t.dim() != 3:
+        raise ValueError(f"{name} must be 3-D")
+    B, rows, width = t.shape
+    N, C = (width, rows) if layout == BCN else (rows, width)
+    if t.is_contiguous():
+        return B, N, C, width
+    s = t.stride()
+    row = s[1] if rows > 1 else s[0] if B > 1 else width
+    if (width > 1 and s[2] != 1) or row < width or (B > 1 and s[0] != rows * row):
+        raise ValueError(f"{name} must be contiguous, or rows that are evenly spaced")
+    return B, N, C, row
+
+
+def _target(target, B, N):
+    if target is not None and tuple(_any(target, "target", (torch.int32,)).shape) != (B, N):
+        raise ValueError("target must be int32 [B,N]")
+
+
+def flexlogp_fwd(logits, target=None, top=0, layout=BCN, workspace=None):
+    """Log softmax of every position's scores at its target (int32 [B,N]; -1: position ignored), entropy, log-sum-exp, and the `top`
+    best log probabilities with their classes.  Returns (logp, entropy, lse [B,N], top_logp, top_class [B,N,top] or
+    [B,top,N]), fp32 and int32; logp is None without target, the last two are None for top = 0."""
+    layout = _layout(layout)
+    B, N, C, row = _score_dims(logits, layout, "logits")
+    _target(target, B, N)
+    top = int(top)
+    need = lib().flexlogp_fwd_workspace_bytes(B, N, C, top, _DTYPES[logits.dtype], layout)
+    if need == 0:
+        raise ValueError(f"flexlogp_fwd does not take B={B}, N={N}, C={C}, top={top}")
+    stats = torch.empty((3, B, N), dtype=torch.float32, device=logits.device)
+    logp, entropy, lse = stats.unbind(0)
+    if target is None:
+        logp = None
+    top_logp = top_class = None
+    if top:
+        shape = (B, top, N) if layout == BCN else (B, N, top)
+        top_logp = torch.empty(shape, dtype=torch.float32, device=logits.device)
+        top_class = torch.empty(shape, dtype=torch.int32, device=logits.device)
+    ws, ws_bytes = _ws_arg(workspace, logits.device, need)
+    _check(lib().flexlogp_fwd(_ptr(logits), _ptr(target), _ptr(logp), _ptr(entropy), _ptr(lse), _ptr(top_logp), _ptr(top_class),
+                              B, N, C, top, row, _DTYPES[logits.dtype], layout, _ptr(ws), ws_bytes, _stream()), "flexlogp_fwd")
+    return logp, entropy, lse, top_logp, top_class
+
+
+def flexlogp_bwd(logits, target, lse, entropy, grad_logp, grad_entropy=None, layout=BCN, out=None):
+    """Gradient of the scores from those of logp and of entropy (either None), with lse and entropy of flexlogp_fwd (entropy may be
+    None without grad_entropy).  Returns grad_logits, shaped like logits; out: where to put it, logits itself for in place."""
+    layout = _layout(layout)
+    B, N, C, row = _score_dims(logits, layout, "logits")
+    _target(target, B, N)
+    if grad_logp is None and grad_entropy is None:
+        raise ValueError("grad_logp and grad_entropy are both None")
+    if (grad_logp is not None and target is None) or (grad_entropy is not None and entropy is None):
+        raise ValueError("grad_logp needs target, grad_entropy needs entropy")
+    for t, name in ((lse, "lse"), (entropy, "entropy"), (grad_logp, "grad_logp"), (grad_entropy, "grad_entropy")):
+        if t is None and name != "lse":
+            continue
+        if tuple(_any(t, name, _F32).shape) != (B, N):
+            raise ValueError(f"{name} must be [B,N]")
+    if out is None:
+        out = torch.empty(logits.shape, dtype=logits.dtype, device=logits.device)
+        grad_row = logits.shape[2]
+    else:
+        grad_row = _score_dims(out, layout, "out")[3]
+        if out.shape != logits.shape or out.dtype != logits.dtype:
+            raise ValueError("out must have the scores' shape and type")
+    _check(lib().flexlogp_bwd(_ptr(logits), _ptr(target), _ptr(lse), _ptr(entropy), _ptr(grad_logp), _ptr(grad_entropy), _ptr(out),
+                              B, N, C, row, grad_row, _DTYPES[logits.dtype], layout, _stream()), "flexlogp_bwd")
+    return out
+
+
+class _AdamwTensor(ctypes.Structure):
+    _fields_ = [(n, _vp) for n in ("param", "exp_avg", "exp_avg_sq", "avg_scale", "avg_sq_scale", "copy")] + \
+               [("count", ctypes.c_int64), ("weight_decay", ctypes.c_double)]
+
+
+class _Adamw(ctypes.Structure):
+    _fields_ = [("plan", _vp), ("chunks", ctypes.c_int64)] + \
+               [(n, ctypes.c_int32) for n in ("tensors", "param_dtype", "state_bits", "copy_dtype")]
+
+
+class AdamWPlan:
+    """An optimizer over fixed tensors, as flexadamw_plan_build makes it; it keeps them alive.  Calls that share one must be
+    stream-ordered."""
+
+    def __init__(self, handle, memory, params, state):
+        self._handle, self._memory, self._state = handle, memory, state
+        self.params = params
+        self._counts = [p.numel() for p in params]
+        self._grads = (_vp * len(params))()
+
+    def steps(self):
+        """The number of steps done (synchronises)."""
+        return int(self._memory[32:40].view(torch.int64).item())       # FLEX_ADAMW_STEPS_AT
+
+
+def flexadamw_state(params, bits=32):
+    """The state before the first step: (exp_avg, exp_avg_sq, avg_scales, avg_sq_scales), lists of tensors of zeros: fp32 and no
+    scales (None), or float8_e4m3fn values with a float8_e8m0fnu power of two for every 32."""
+    if bits not in (8, 32):
+        raise ValueError("bits must be 8 or 32")
+    if bits == 32:
+        return [torch.zeros_like(p, dtype=torch.float32) for p in params], [torch.zeros_like(p, dtype=torch.float32) for p in params], None, None
+    zeros = lambda n, p, dtype: torch.zeros(n, dtype=torch.uint8, device=p.device).view(dtype)
+    values = lambda: [zeros(p.numel(), p, torch.float8_e4m3fn).view(p.shape) for p in params]
+    scales = lambda: [zeros((p.numel() + 31) // 32, p, torch.float8_e8m0fnu) for p in params]
+    return values(), values(), scales(), scales()
+
+
+def flexadamw_plan_build(params, exp_avg, exp_avg_sq, avg_scales=None, avg_sq_scales=None, copies=None, weight_decay=0.0,
+                         betas=(0.9, 0.999), eps=1e-8, steps=0, seed=0):
+    """An AdamWPlan for flexadamw_step over `params` (one type: fp32, bf16 or fp16) with states as flexadamw_state makes them, updated
+    in place.  copies: bf16 or fp16 tensors that get the new values too; weight_decay: a number, or one for each tensor;
+    steps: how many were done before."""
+    params, exp_avg, exp_avg_sq = list(params), list(exp_avg), list(exp_avg_sq)
+    n = len(params)
+    if n == 0:
+        raise ValueError("no parameters")
+    eight = avg_scales is not None
+    if eight != (avg_sq_scales is not None):
+        raise ValueError("avg_scales and avg_sq_scales: both or neither")
+    decay = [float(d) for d in weight_decay] if isinstance(weight_decay, (list, tuple)) else [float(weight_decay)] * n
+    lists = [("exp_avg", exp_avg), ("exp_avg_sq", exp_avg_sq), ("weight_decay", decay)]
+    avg_scales, avg_sq_scales = list(avg_scales or []), list(avg_sq_scales or [])
+    copies = list(copies) if copies is not None else None
+    lists += [("avg_scales", avg_scales), ("avg_sq_scales", avg_sq_scales)] if eight else []
+    lists += [("copies", copies)] if copies is not None else []
+    for name, got in lists:
+        if len(got) != n:
+            raise ValueError(f"{name}: {len(got)} entries for {n} parameters")
+    ptype, spans = params[0].dtype if isinstance(params[0], torch.Tensor) else None, []
+    ctype = copies[0].dtype if copies and isinstance(copies[0], torch.Tensor) else torch.bfloat16
+    entries = (_AdamwTensor * n)()
+    for i, p in enumerate(params):
+        _any(p, f"params[{i}]", (ptype,) if ptype in _DTYPES else _DTYPES)
+        parts = [(p, "params")]
+        for name, got in (("exp_avg", exp_avg), ("exp_avg_sq", exp_avg_sq)):
+            if _any(got[i], f"{name}[{i}]", (torch.float8_e4m3fn,) if eight else _F32).numel() != p.numel():
+                raise ValueError(f"{name}[{i}] must have as many elements as its parameter")
+            parts.append((got[i], name))
+        if eight:
+            for name, got in (("avg_scales", avg_scales), ("avg_sq_scales", avg_sq_scales)):
+                if _any(got[i], f"{name}[{i}]", (torch.float8_e8m0fnu,)).numel() != (p.numel() + 31) // 32:
+                    raise ValueError(f"{name}[{i}] must have an element for every 32 of its parameter's")
+                parts.append((got[i], name))
+        if copies is not None:
+            if ctype not in (torch.bfloat16, torch.float16) or _any(copies[i], f"copies[{i}]", (ctype,)).numel() != p.numel():
+                raise ValueError(f"copies[{i}] must be bf16 or fp16, like the first, with as many elements as its parameter")
+            parts.append((copies[i], "copies"))
+        spans += [(t.data_ptr(), t.data_ptr() + t.numel() * t.element_size(), f"{name}[{i}]") for t, name in parts if t.numel()]
+        entries[i] = _AdamwTensor(_ptr(p), _ptr(exp_avg[i]), _ptr(exp_avg_sq[i]), _ptr(avg_scales[i]) if eight else None,
+                                  _ptr(avg_sq_scales[i]) if eight else None, None if copies is None else _ptr(copies[i]),
+                                  p.numel(), decay[i])
+    spans.sort()
+    for (_, end, one), (begin, _, other) in zip(spans, spans[1:]):
+        if begin < end:
+            raise ValueError(f"{one} and {other} share memory")
+    need = lib().flexadamw_plan_bytes(entries, n)
+    if need == 0:
+        raise ValueError("sizes out of range")
+    memory = torch.empty(need, dtype=torch.uint8, device=params[0].device)
+    handle = _Adamw()
+    _check(lib().flexadamw_plan_build(entries, n, _DTYPES[params[0].dtype], 8 if eight else 32, _DTYPES[ctype], float(betas[0]),
+                                      float(betas[1]), float(eps), int(steps), int(seed) & 0xFFFFFFFF, _ptr(memory), need,
+                                      ctypes.byref(handle), _stream()), "flexadamw_plan_build")
+    return AdamWPlan(handle, memory, params, (exp_avg, exp_avg_sq, avg_scales, avg_sq_scales, copies))
+
+
+def flexadamw_step(plan, grads, lr, grad_scale=None):
+    """One AdamW step of plan's tensors, in place.  grads: a tensor of its parameter's size for each (one type), None: left as it is.
+    lr: a number, or an fp32 CUDA tensor of one element; grad_scale: such a tensor, multiplied onto the gradients; where it is not finite
+    the step is left out."""
+    grads = list(grads)
+    counts, dtype = plan._counts, None
+    if len(grads) != len(counts):
+        raise ValueError(f"{len(grads)} gradients for {len(counts)} parameters")
+    device = plan._memory.device
+    if device.index != torch.cuda.current_device():
+        raise ValueError(f"the plan is on {device}, the current device is cuda:{torch.cuda.current_device()}")
+    at = plan._grads
+    for i, g in enumerate(grads):
+        if g is None:
+            at[i] = None
+            continue
+        if dtype is None and isinstance(g, torch.Tensor):
+            dtype = g.dtype
+            if dtype not in _DTYPES:
+                raise TypeError(f"grads[{i}] must be fp32, bf16 or fp16, got {dtype}")
+        if not isinstance(g, torch.Tensor) or g.device != device or g.dtype != dtype:
+            raise TypeError(f"grads[{i}] must be a {dtype} tensor on {device}")
+        if g.numel() != counts[i] or not g.is_contiguous():
+            raise ValueError(f"grads[{i}] must be contiguous with {counts[i]} elements")
+        at[i] = g.data_ptr()
+    for t, name in ((lr if isinstance(lr, torch.Tensor) else None, "lr"), (grad_scale, "grad_scale")):
+        if t is not None and _any(t, name, _F32).numel() != 1:
+            raise ValueError(f"{name} must have one element")
+    number, at_lr = (0.0, _ptr(lr)) if isinstance(lr, torch.Tensor) else (float(lr), None)
+    _check(lib().flexadamw_step(ctypes.byref(plan._handle), at, len(counts), _DTYPES.get(dtype, 0), number, at_lr, _ptr(grad_scale),
+                                _stream()), "flexadamw_step")
 
 
 def flex_calibrate_copy(src, dst):

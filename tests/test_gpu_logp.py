@@ -1,0 +1,201 @@
+"""Log probabilities, entropy, alternatives and the scores' gradient on the GPU against float64."""
+import numpy as np
+import pytest
+import torch
+
+import paper_1803_07289_amd as fx
+from oracle import operators as ref
+from gpu_util import say
+from operator_util import TYPES, U, chain, half_step, laid_out, smallest_half, to_positions, within
+
+pytestmark = pytest.mark.gpu
+
+#         B, N, C, top
+SHAPES = [(1, 1, 1, 1), (1, 3, 2, 2), (2, 5, 3, 3), (1, 130, 7, 1), (1, 1000, 13, 3), (3, 67, 16, 5), (1, 200, 33, 32), (2, 31, 50, 8),
+          (1, 64, 64, 4), (1, 33, 65, 20), (1, 77, 129, 3), (1, 20, 255, 32), (2, 9, 513, 8), (1, 12, 1000, 20), (1, 5, 4097, 32),
+          (1, 3, 16385, 7), (1, 2, 50001, 20), (2, 1, 131072, 32), (1, 1, 200003, 0), (1, 1, 1 << 20, 5), (1, 300, 100, 0)]
+
+
+def scores(seed, rows, C, dtype, spread=3.0):
+    rng = np.random.default_rng(seed)
+    return rng, torch.from_numpy(rng.standard_normal((rows, C)) * spread).to(dtype).double().numpy()
+
+
+def check_fwd(x, t, got, top, layout):
+    logp, h, lse, top_logp, top_class = got
+    wlogp, wh, wlse, wtop, wclass = ref.logp_fwd(x, t, top)
+    flat = lambda v: v.double().cpu().numpy().reshape(-1)
+    live = np.isfinite(wlse) & (np.ones(len(x), bool) if t is None else (np.asarray(t) >= 0) & (np.asarray(t) < x.shape[1]))
+    # exp(z), z = x - max: z and its product with log2(e) are rounded, 1.5 U |z| log2(e) of the exponent each, and the power itself: 2 U;
+    # weighted by p that is the relative error of the sum, beside its own additions
+    with np.errstate(all="ignore"):
+        z = np.where(live[:, None], x - np.max(x, 1, keepdims=True), 0.0)
+        p = np.where(np.isneginf(z), 0.0, np.exp(np.where(live[:, None], x - wlse[:, None], -np.inf)))
+        zs = np.where(np.isneginf(z), 0.0, np.abs(z))
+    k = (p * (3 * zs + 4)).sum(1) * U + chain(x.shape[1], 64)
+    log_s = np.where(live, wlse - np.where(live, np.max(x, 1), 0), 0)
+    b_lse = k + 4 * U * (np.abs(log_s) + np.abs(np.where(live, wlse, 0)))
+    within(flat(lse), wlse, b_lse, "lse")
+    # entropy = log s - u / s: u's terms carry the errors of exp and of z
+    within(flat(h), wh, 2 * k * (1 + (p * zs).sum(1)) + (p * zs * (3 * zs + 8)).sum(1) * U + 4 * U * np.abs(log_s), "entropy")
+    if t is not None:
+        within(flat(logp), wlogp, b_lse + 4 * U * np.abs(np.where(np.isfinite(wlogp), wlogp, 0)), "logp")
+    if top:
+        assert np.array_equal(to_positions(top_class, layout).astype(np.int32), wclass), "classes"
+        within(to_positions(top_logp, layout), wtop, b_lse[:, None] + 4 * U * np.abs(np.where(np.isfinite(wtop), wtop, 0)), "top_logp")
+    else:
+        assert top_logp is None and top_class is None
+
+
+def check_bwd(x, t, lse, h, gl, gh, got, dtype, layout):
+    want = ref.logp_bwd(x, t, lse, h, gl, gh)
+    with np.errstate(all="ignore"):
+        lp = np.where(np.isfinite(x) & np.isfinite(lse)[:, None], x - lse[:, None], 0.0)
+        p = np.where(np.isfinite(x) & np.isfinite(lse)[:, None], np.exp(lp), 0.0)
+    part = 0 if gl is None else np.abs(gl)[:, None]
+    part = part + (0 if gh is None else np.abs(gh)[:, None] * (np.abs(lp) + np.abs(h)[:, None]))
+    # the exponent's roundings 3 U |lp|, the power's 2 U, and those of the products
+    bound = p * part * (3 * np.abs(lp) + 10) * U + (0 if gl is None else 2 * U * np.abs(gl)[:, None])
+    within(to_positions(got, layout), want, bound + half_step(dtype) * np.abs(want) + smallest_half(dtype), "grad_logits")
+
+
+@pytest.mark.parametrize("layout", [fx.BNC, fx.BCN], ids=["bnc", "bcn"])
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("shape", SHAPES, ids=str)
+def test_log_probabilities(shape, dtype, layout):
+    B, N, C, top = shape
+    say(f"logp {shape} {dtype} {layout}")
+    td = TYPES[dtype]
+    rows = B * N
+    rng, x = scores(sum(shape), rows, C, td)
+    if C > 2:
+        x[rng.random((rows, C)) < 0.1] = -np.inf
+    if rows > 4:
+        x[1] = -np.inf                                                # nothing left
+        x[2] = -np.inf
+        x[2, C - 1] = 1.0                                             # one class left
+        x[3] = np.round(x[3])                                         # ties
+    t = rng.integers(0, C, rows)
+    if rows > 6:
+        t[4:6] = -1
+        t[6] = C                                                      # no class either
+        x[5] = np.nan                                                 # not looked at
+    offset, pad = sum(shape) % 3, (0, 3, 8)[sum(shape) % 3]
+    dx = laid_out(x, B, layout, td, offset, (N if layout == fx.BCN else C) + pad)
+    dt = torch.from_numpy(t.astype(np.int32)).view(B, N).cuda()
+    need = fx.lib().flexlogp_fwd_workspace_bytes(B, N, C, top, fx._DTYPES[td], layout)
+    guarded = torch.full((need + 4096,), 0xA5, dtype=torch.uint8, device="cuda")
+    got = fx.flexlogp_fwd(dx, dt, top=top, layout=layout, workspace=guarded[:need])
+    check_fwd(x, t, got, top, layout)
+    assert bool((guarded[need:] == 0xA5).all()), "wrote past the workspace"
+    free = np.setdiff1d(np.arange(rows), [5]) if rows > 6 else np.arange(rows)
+    bare = fx.flexlogp_fwd(dx, top=top, layout=layout)
+    assert bare[0] is None
+    pick = lambda v: None if v is None else to_positions(v, layout)[free]
+    sub = lambda v: v.reshape(-1)[torch.from_numpy(free).cuda()]
+    tl, tc = (None, None) if not top else (torch.from_numpy(pick(bare[3])), torch.from_numpy(pick(bare[4])))
+    if top:
+        tl, tc = tl[None], tc[None]
+    check_fwd(x[free], None, (None, sub(bare[1]), sub(bare[2]), tl, tc), top, fx.BNC)
+
+    lse, h = got[2].double().cpu().numpy().reshape(-1), got[1].double().cpu().numpy().reshape(-1)
+    f32 = lambda a: a.astype(np.float32).astype(np.float64)
+    gl, gh = f32(rng.standard_normal(rows)), f32(rng.standard_normal(rows))
+    d = lambda a: torch.from_numpy(a.astype(np.float32)).view(B, N).cuda()
+    for a, b in ((gl, gh), (gl, None), (None, gh)):
+        gx = fx.flexlogp_bwd(dx, dt, got[2], got[1], None if a is None else d(a), None if b is None else d(b), layout=layout)
+        check_bwd(x, t, lse, h, a, b, gx, td, layout)
+    same = dx.clone() if dx.is_contiguous() else laid_out(x, B, layout, td, offset, (N if layout == fx.BCN else C) + pad)
+    two = fx.flexlogp_bwd(same, dt, got[2], None, d(gl), layout=layout, out=same)            # in place
+    assert two.data_ptr() == same.data_ptr()
+    check_bwd(x, t, lse, h, gl, None, two, td, layout)
+
+
+@pytest.mark.parametrize("layout", [fx.BNC, fx.BCN], ids=["bnc", "bcn"])
+def test_elements_between_rows_of_the_gradient_stay(layout):
+    _, x = scores(1, 60, 13, torch.float32)
+    lse = torch.logsumexp(torch.from_numpy(x), 1).float().view(2, 30).cuda()
+    t = torch.zeros(2, 30, dtype=torch.int32, device="cuda")
+    wide = torch.full((2, 13, 40) if layout == fx.BCN else (2, 30, 20), 7.0, device="cuda")
+    out = wide[:, :, :30 if layout == fx.BCN else 13]
+    fx.flexlogp_bwd(laid_out(x, 2, layout, torch.float32), t, lse, None, torch.ones(2, 30, device="cuda"), layout=layout, out=out)
+    assert bool((wide[:, :, out.shape[2]:] == 7).all())
+    check_bwd(x, np.zeros(60, int), lse.double().cpu().numpy().reshape(-1), None, np.ones(60), None, out, torch.float32, layout)
+
+
+@pytest.mark.parametrize("layout", [fx.BNC, fx.BCN], ids=["bnc", "bcn"])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("C", [5, 40, 700, 5000, 40000])
+def test_rows_that_are_all_alike_take_the_lowest_classes(C, dtype, layout):
+    """Every class a candidate: ties everywhere, ascending and descending rows, the best ones all in one place."""
+    top = min(C, 32)
+    x = np.zeros((6, C))
+    x[1] = np.arange(C) * (64.0 / C)
+    x[2] = -np.arange(C) * (64.0 / C)
+    x[3, C // 2:C // 2 + top] = 5.0
+    x[4] = np.arange(C) // 8 % 2
+    x[5, 1::2] = -np.inf
+    x = torch.from_numpy(x).to(TYPES[dtype]).double().numpy()
+    dx = laid_out(x, 1, layout, TYPES[dtype])
+    check_fwd(x, None, fx.flexlogp_fwd(dx, top=top, layout=layout), top, layout)
+
+
+@pytest.mark.parametrize("layout", [fx.BNC, fx.BCN], ids=["bnc", "bcn"])
+@pytest.mark.parametrize("C", [9, 300, 3000, 70000])
+def test_nan_and_infinity_among_the_scores(C, layout):
+    _, x = scores(4, 4, C, torch.float32)
+    x[1, C // 3] = np.nan
+    x[2, C // 2] = np.inf
+    got = fx.flexlogp_fwd(laid_out(x, 1, layout, torch.float32), torch.zeros(1, 4, dtype=torch.int32, device="cuda"), top=4, layout=layout)
+    for v in got[:3]:
+        assert torch.isnan(v[0, 1:3]).all() and torch.isfinite(v[0, [0, 3]]).all()
+    classes = to_positions(got[4], layout).astype(int)
+    order = np.lexsort((np.arange(C), -np.where(np.isnan(x[1]), -np.inf, x[1])))[:4]
+    assert classes[1].tolist() == order.tolist() and classes[2, 0] == C // 2
+    check_fwd(x[[0, 3]], None, (None,) + tuple(v[:, [0, 3]] for v in got[1:3]) + tuple(
+        torch.from_numpy(to_positions(v, layout)[[0, 3]])[None] for v in got[3:]), 4, fx.BNC)
+
+
+def test_scores_of_the_types_extremes():
+    big = float(torch.finfo(torch.float32).max)
+    x = np.array([[-big, 0.0, 1.0, -big], [-big] * 4, [big, big, 0.0, -big], [88.0, -88.0, 700.0, 699.0]])
+    x = x.astype(np.float32).astype(np.float64)
+    t = torch.tensor([[2, 1, 0, 3]], dtype=torch.int32, device="cuda")
+    got = fx.flexlogp_fwd(laid_out(x, 1, fx.BNC, torch.float32), t, top=2, layout=fx.BNC)
+    ln = np.log
+    assert np.allclose(got[0].cpu().numpy(), [[-ln(1 + np.exp(-1)), -ln(4), -ln(2), -1 - ln(1 + np.exp(-1))]], atol=1e-6)
+    assert got[4][0].cpu().tolist() == [[2, 1], [0, 1], [0, 1], [2, 3]]
+    assert np.allclose(got[1].cpu().numpy()[0, 1:3], [ln(4), ln(2)], atol=1e-6)
+
+
+def test_rows_beyond_32_bit_offsets():
+    """More than 2^32 elements of scores, the last rows looked at."""
+    N, C = 17_000, 260_000
+    x = torch.empty(1, N, C, dtype=torch.bfloat16, device="cuda")
+    x[:, :-3].fill_(-1.0)
+    rng, tail = scores(8, 3, C, torch.bfloat16)
+    x[0, -3:] = torch.from_numpy(tail).to(torch.bfloat16).cuda()
+    t = torch.full((1, N), -1, dtype=torch.int32, device="cuda")
+    t[0, -3:] = torch.tensor([5, C - 1, 1000], dtype=torch.int32)
+    got = fx.flexlogp_fwd(x, t, top=3, layout=fx.BNC)
+    check_fwd(tail, [5, C - 1, 1000], tuple(v[:, -3:] for v in got), 3, fx.BNC)
+    assert bool((got[0][0, :-3] == 0).all()) and bool((got[4][0, :-3] == -1).all())
+    gl = torch.ones(1, N, device="cuda")
+    gx = fx.flexlogp_bwd(x, t, got[2], None, gl, layout=fx.BNC, out=x)
+    check_bwd(tail, [5, C - 1, 1000], got[2][0, -3:].double().cpu().numpy(), None, np.ones(3), None, gx[:, -3:], torch.bfloat16, fx.BNC)
+    assert float(gx[0, :-3].abs().amax()) == 0.0
+
+
+def test_refusals_of_the_binding():
+    x, t = torch.zeros(2, 5, 8, device="cuda"), torch.zeros(2, 5, dtype=torch.int32, device="cuda")
+    logp, h, lse, _, _ = fx.flexlogp_fwd(x, t, layout=fx.BNC)
+    f = lambda *a, **k: (lambda: fx.flexlogp_fwd(*a, layout=fx.BNC, **k))
+    g = lambda *a, **k: (lambda: fx.flexlogp_bwd(*a, layout=fx.BNC, **k))
+    for call, error in ((f(x[0], t), ValueError), (f(x, t.long()), TypeError), (f(x, t[:1]), ValueError), (f(x, t, top=9), ValueError),
+                        (f(x, t, top=-1), ValueError), (f(x.double(), t), TypeError), (f(x.transpose(1, 2), t), ValueError),
+                        (f(x[:, :, ::2], t), ValueError), (f(x[:, :1].expand(2, 5, 8), t), ValueError), (f(x[:, ::2, :], t[:, ::2]), ValueError),
+                        (g(x, t, lse, h, None, None), ValueError), (g(x, None, lse, h, lse), ValueError), (g(x, t, lse, None, lse, lse), ValueError),
+                        (g(x, t, lse[:, :3], h, lse), ValueError), (g(x, t, lse, h, lse, out=x[:, :, :7]), ValueError),
+                        (g(x, t, lse, h, lse, out=x.half()), ValueError)):
+        with pytest.raises(error):
+            call()
