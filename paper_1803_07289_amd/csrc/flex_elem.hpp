@@ -1,5 +1,5 @@
 // Element types of the operators around the layers (layer norm, log probabilities, optimizer step): fp32, bf16 and fp16
-// tensors, computed on in fp32.
+// tensors, computed on in fp32; rows read 16 bytes a lane; reductions over the lanes that share a row.
 #pragma once
 #include "flex_common.hpp"
 #include "../../include/flexconv.h"
@@ -21,6 +21,90 @@ static inline hipError_t with_dtype(int d, F f)
     if (d == FLEX_F32) return f(float{});
     if (d == FLEX_BF16) return f(bf16{});
     return f(_Float16{});
+}
+
+// Elements a lane takes at once; rows may begin at any element (the hardware takes any alignment, and a row's lines are the same).
+template <class T>
+constexpr int LANE_ELEMENTS = 16 / (int)sizeof(T);
+template <class T, int N = LANE_ELEMENTS<T>>
+struct Chunk {
+    typedef T V __attribute__((ext_vector_type(N), aligned(sizeof(T))));
+    static __device__ __forceinline__ void load(const T *p, float (&x)[N])
+    {
+        const V v = *(const V *)p;
+#pragma unroll
+        for (int j = 0; j < N; ++j) x[j] = to_f32(v[j]);
+    }
+    static __device__ __forceinline__ void store(T *p, const float (&x)[N])
+    {
+        V v;
+#pragma unroll
+        for (int j = 0; j < N; ++j) v[j] = (T)x[j];
+        *(V *)p = v;
+    }
+    // columns c0 .. of a row of C, `fill` behind its end
+    static __device__ __forceinline__ void load_row(const T *row, int c0, int C, float (&x)[N], float fill)
+    {
+        if (c0 + N <= C) load(row + c0, x);
+        else
+#pragma unroll
+            for (int j = 0; j < N; ++j) x[j] = c0 + j < C ? to_f32(row[c0 + j]) : fill;
+    }
+    static __device__ __forceinline__ void store_row(T *row, int c0, int C, const float (&x)[N])
+    {
+        if (c0 + N <= C) store(row + c0, x);
+        else
+#pragma unroll
+            for (int j = 0; j < N; ++j)
+                if (c0 + j < C) row[c0 + j] = (T)x[j];
+    }
+};
+
+// ---- reductions over groups of L neighbouring lanes, the result on every one of them -----------------------------------------
+// Up to 16 lanes by DPP (quad permutes, then the mirrored half row and row, whose halves hold one value each by then); all lanes of
+// a group have to be active.
+
+template <int CTRL>
+__device__ __forceinline__ float dpp_f32(float v)
+{
+    return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CTRL, 0xF, 0xF, true));
+}
+template <int CTRL>
+__device__ __forceinline__ int dpp_i32(int v) { return __builtin_amdgcn_update_dpp(0, v, CTRL, 0xF, 0xF, true); }
+
+constexpr int DPP_XOR1 = 0xB1, DPP_XOR2 = 0x4E, DPP_HALF_MIRROR = 0x141, DPP_MIRROR = 0x140;
+
+template <int L, class Op>
+__device__ __forceinline__ float lanes_reduce(float v, Op op)
+{
+    if (L >= 2) v = op(v, dpp_f32<DPP_XOR1>(v));
+    if (L >= 4) v = op(v, dpp_f32<DPP_XOR2>(v));
+    if (L >= 8) v = op(v, dpp_f32<DPP_HALF_MIRROR>(v));
+    if (L >= 16) v = op(v, dpp_f32<DPP_MIRROR>(v));
+    if (L >= 32) v = op(v, __shfl_xor(v, 16));
+    if (L >= 64) v = op(v, __shfl_xor(v, 32));
+    return v;
+}
+template <int L>
+__device__ __forceinline__ float lanes_sum(float v)
+{
+    return lanes_reduce<L>(v, [](float a, float b) { return a + b; });
+}
+template <int L>
+__device__ __forceinline__ float lanes_max(float v)
+{
+    return lanes_reduce<L>(v, [](float a, float b) { return fmaxf(a, b); });
+}
+template <int L>
+__device__ __forceinline__ int lanes_min(int v)
+{
+    if (L >= 2) v = min(v, dpp_i32<DPP_XOR1>(v));
+    if (L >= 4) v = min(v, dpp_i32<DPP_XOR2>(v));
+    if (L >= 8) v = min(v, dpp_i32<DPP_HALF_MIRROR>(v));
+    if (L >= 16) v = min(v, dpp_i32<DPP_MIRROR>(v));
+    if (L >= 32) v = min(v, __shfl_xor(v, 16));
+    if (L >= 64) v = min(v, __shfl_xor(v, 32));
+    return v;
 }
 
 // a vector over the channels in a parameter type that is known at run time (read rarely: once a workgroup, or from a cache)

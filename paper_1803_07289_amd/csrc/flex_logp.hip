@@ -4,79 +4,414 @@
 //   p = exp(x - lse):  grad_x = grad_logp ([c = t] - p) - grad_H p (x - lse + H)
 // A score of -inf has p = 0 and no share of anything; positions whose target is no class are ignored (outputs zero, no
 // alternatives, gradient zero, scores not looked at); one without any score above -inf has logp = lse = -inf, H = 0.
+//
+// Every kernel reads a score once and keeps it in a register, fp32 or packed as it was, until its position is done: the maximum, the
+// two sums and the alternatives all come from there.
 #include "flex_elem.hpp"
+#include <algorithm>
 
 namespace flex {
 
 constexpr float LOG2E = 1.4426950408889634f;
 constexpr float MASKED = -1e5f;       // stands for x - m = -inf where it is multiplied by exp(x - m) = 0
+constexpr int NO_CLASS = 0x7FFFFFFF;
 
 struct LogpArgs {
     const int32_t *target;
     float *logp, *entropy, *lse, *top_logp;
     int32_t *top_class;
     int64_t rows, bs, ps, cs;         // positions; element strides: cloud, position, class
-    int N, C, top, bcn;
+    int N, C, top;
 };
 
-template <class T>
-__global__ __launch_bounds__(256) void logp_fwd_kernel(const T *__restrict__ x, LogpArgs a)
+struct Sums {
+    float m, s, u;
+};
+// sums about a.m and b.m as one
+__device__ __forceinline__ Sums joined(const Sums &a, const Sums &b)
 {
-    const int lane = threadIdx.x & 63;
-    const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-    if (row >= a.rows) return;
-    const int64_t b = row / a.N, n = row % a.N;
-    const T *at = x + b * a.bs + n * a.ps;
-    const int64_t top_at = a.bcn ? b * a.top * a.N + n : row * a.top, top_step = a.bcn ? a.N : 1;
+    const float m = fmaxf(a.m, b.m);
+    if (m == -INFINITY) return Sums{m, a.s + b.s, 0.f};
+    const float da = fmaxf(a.m - m, MASKED), db = fmaxf(b.m - m, MASKED);
+    const float ea = __builtin_amdgcn_exp2f(da * LOG2E), eb = __builtin_amdgcn_exp2f(db * LOG2E);
+    return Sums{m, a.s * ea + b.s * eb, (a.u + a.s * da) * ea + (b.u + b.s * db) * eb};
+}
+__device__ __forceinline__ void add_score(Sums &a, float x, float m)
+{
+    const float z = x - m, e = __builtin_amdgcn_exp2f(z * LOG2E);
+    a.s += e;
+    a.u += e * fmaxf(z, MASKED);
+}
+// m as the sums are taken about it: an empty position's is no number to subtract
+__device__ __forceinline__ float centre(float m) { return m == -INFINITY ? 0.f : m; }
+
+__device__ __forceinline__ void store_sums(const LogpArgs &a, int64_t row, float target_score, const Sums &k, float log_s)
+{
+    if (a.target) a.logp[row] = k.s == 0.f ? -INFINITY : target_score - k.m - log_s;
+    a.entropy[row] = k.s == 0.f ? 0.f : log_s - k.u / k.s;
+    a.lse[row] = k.m + log_s;
+}
+__device__ __forceinline__ void store_top(const LogpArgs &a, int64_t at, float v, int c, const Sums &k, float log_s)
+{
+    a.top_logp[at] = v == -INFINITY ? -INFINITY : v - k.m - log_s;
+    a.top_class[at] = v == -INFINITY ? -1 : c;
+}
+__device__ __forceinline__ bool ignored(const LogpArgs &a, int t) { return a.target && (t < 0 || t >= a.C); }
+
+// ---- point-major, rows of up to 64 lanes' elements ------------------------------------------------------------------------
+// L lanes hold a row, U times 16 bytes each.  The best score is the maximum over the lanes, its class the smallest among those that
+// hold it; it is then taken out, and so on for each alternative: 2 log2 L steps and three operations an element each.
+template <class T, int L, int U>
+__global__ __launch_bounds__(256) void logp_rows_kernel(const T *__restrict__ x, LogpArgs a)
+{
+    constexpr int N = LANE_ELEMENTS<T>;
+    const int sub = threadIdx.x % L;
+    const int64_t row = (int64_t)blockIdx.x * (256 / L) + threadIdx.x / L;
+    const bool mine = row < a.rows;
+    const int t = mine && a.target ? a.target[row] : 0;
+    const bool skip = !mine || ignored(a, t);
+    const T *at = x + row / a.N * a.bs + row % a.N * a.ps;
+    float v[U][N];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        if (skip)
+#pragma unroll
+            for (int j = 0; j < N; ++j) v[u][j] = -INFINITY;
+        else
+            Chunk<T>::load_row(at, (u * L + sub) * N, a.C, v[u], -INFINITY);
+    }
+    const float target_score = !skip && sub == 0 && a.target ? to_f32(at[t]) : 0.f;
+    float best = -INFINITY;
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int j = 0; j < N; ++j) best = fmaxf(best, v[u][j]);
+    best = lanes_max<L>(best);
+    Sums k{centre(best), 0.f, 0.f};
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int j = 0; j < N; ++j) add_score(k, v[u][j], k.m);
+    k.s = lanes_sum<L>(k.s);
+    k.u = lanes_sum<L>(k.u);
+    const float log_s = logf(k.s);
+    if (mine && sub == 0) {
+        if (skip) {
+            a.logp[row] = a.entropy[row] = a.lse[row] = 0.f;
+        } else
+            store_sums(a, row, target_score, k, log_s);
+    }
+    for (int i = 0; i < a.top; ++i) {
+        int c = NO_CLASS;
+#pragma unroll
+        for (int u = U - 1; u >= 0; --u)
+#pragma unroll
+            for (int j = N - 1; j >= 0; --j)
+                if (v[u][j] == best) c = (u * L + sub) * N + j;
+        c = lanes_min<L>(c);
+        if (mine && sub == i % L) store_top(a, row * a.top + i, best, c, k, log_s);
+        if (i + 1 == a.top) break;
+        best = -INFINITY;
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int j = 0; j < N; ++j) {
+                if ((u * L + sub) * N + j == c) v[u][j] = -INFINITY;
+                best = fmaxf(best, v[u][j]);
+            }
+        best = lanes_max<L>(best);
+    }
+}
+
+// ---- point-major, longer rows ---------------------------------------------------------------------------------------------
+// A workgroup holds a part of a row, 256 x U x 16 bytes, in registers.  Alternatives: the `top`-th largest of a wave's 64 lane maxima
+// bounds the part's `top`-th largest score from below, and so does the largest of the four waves' bounds; what reaches it,
+// little more than `top` scores in most rows, goes to a list in LDS and is ranked there.  A list that overflows (rows full of equal
+// scores) is left for `top` rounds over the registers.  Parts of one row meet in logp_join_kernel.
+constexpr int PART_LIST = 512;
+
+// the bits of a float, ordered like the floats
+__device__ __forceinline__ uint32_t order_key(float v)
+{
+    const uint32_t b = __builtin_bit_cast(uint32_t, v);
+    return b ^ ((uint32_t)((int32_t)b >> 31) | 0x80000000u);
+}
+__device__ __forceinline__ float from_order_key(uint32_t k)
+{
+    return __builtin_bit_cast(float, k ^ (k >> 31 ? 0x80000000u : 0xFFFFFFFFu));
+}
+
+// A value that at least n of the wave's 64 lanes reach, the largest such one to within the last 12 bits; -inf if fewer are above -inf.
+__device__ __forceinline__ float reached_by(float v, int n)
+{
+    const uint32_t key = order_key(v);
+    uint32_t found = 0;
+#pragma unroll
+    for (int b = 31; b >= 12; --b) {
+        const uint32_t next = found | 1u << b;
+        if (__popcll(__ballot(key >= next)) >= n) found = next;
+    }
+    return found <= order_key(-INFINITY) ? -INFINITY : from_order_key(found);
+}
+
+// What a part leaves of itself: its sums and its best scores with their classes.
+struct LogpParts {
+    Sums *sums;                       // [rows][parts], 16 bytes apart
+    float2 *best;                     // [rows][parts][top]: score, class (as bits)
+    int parts;
+};
+constexpr int SUMS_BYTES = 16;
+
+template <class T, int U>
+__global__ __launch_bounds__(256) void logp_part_kernel(const T *__restrict__ x, LogpArgs a, LogpParts p)
+{
+    constexpr int N = LANE_ELEMENTS<T>;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int64_t row = blockIdx.x / p.parts;
+    const int part = (int)(blockIdx.x % p.parts);
     const int t = a.target ? a.target[row] : 0;
-    if (a.target && (t < 0 || t >= a.C)) {
-        if (lane == 0) a.logp[row] = a.entropy[row] = a.lse[row] = 0.f;
-        if (lane < a.top) {
-            a.top_logp[top_at + lane * top_step] = -INFINITY;
-            a.top_class[top_at + lane * top_step] = -1;
+    if (ignored(a, t)) {
+        if (part == 0) {
+            if (tid == 0) a.logp[row] = a.entropy[row] = a.lse[row] = 0.f;
+            if (tid < a.top) {
+                a.top_logp[row * a.top + tid] = -INFINITY;
+                a.top_class[row * a.top + tid] = -1;
+            }
         }
         return;
     }
-    float m = -INFINITY, s = 0.f, u = 0.f;
-    for (int c = lane; c < a.C; c += 64) m = fmaxf(m, to_f32(at[c * a.cs]));
-    m = wave_max(m);
-    if (m == -INFINITY) m = 0.f;
-    for (int c = lane; c < a.C; c += 64) {
-        const float z = to_f32(at[c * a.cs]) - m, e = __builtin_amdgcn_exp2f(z * LOG2E);
-        s += e;
-        u += e * fmaxf(z, MASKED);
-    }
-    s = wave_sum(s);
-    u = wave_sum(u);
-    const float log_s = logf(s);
-    if (lane == 0) {
-        if (a.target) a.logp[row] = s == 0.f ? -INFINITY : to_f32(at[t * a.cs]) - m - log_s;
-        a.entropy[row] = s == 0.f ? 0.f : log_s - u / s;
-        a.lse[row] = m + log_s;
-    }
-    float last = INFINITY;
-    int last_c = -1;
-    for (int k = 0; k < a.top; ++k) {       // the best of those behind the last one found
-        float best = -INFINITY;
-        int best_c = INT_MAX;
-        for (int c = lane; c < a.C; c += 64) {
-            const float v = to_f32(at[c * a.cs]);
-            if (v > best && (v < last || (v == last && c > last_c))) { best = v; best_c = c; }
-        }
+    __shared__ Sums s_sums[4];
+    __shared__ float s_bound[4], s_best[4];
+    __shared__ int s_count, s_class[4];
+    __shared__ float s_value[PART_LIST];
+    __shared__ int s_from[PART_LIST];
+    const T *at = x + row / a.N * a.bs + row % a.N * a.ps;
+    const int c0 = part * (256 * N * U) + tid * N;
+    float v[U][N];
 #pragma unroll
-        for (int o = 32; o > 0; o >>= 1) {
-            const float v = __shfl_xor(best, o);
-            const int c = __shfl_xor(best_c, o);
-            if (v > best || (v == best && c < best_c)) { best = v; best_c = c; }
+    for (int u = 0; u < U; ++u) Chunk<T>::load_row(at, c0 + u * 256 * N, a.C, v[u], -INFINITY);
+    const float target_score = tid == 0 && a.target && p.parts == 1 ? to_f32(at[t]) : 0.f;
+    float most[U], best = -INFINITY;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        most[u] = v[u][0];
+#pragma unroll
+        for (int j = 1; j < N; ++j) most[u] = fmaxf(most[u], v[u][j]);
+        best = fmaxf(best, most[u]);
+    }
+    Sums k{lanes_max<64>(best), 0.f, 0.f};
+    const float m = centre(k.m);
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int j = 0; j < N; ++j) add_score(k, v[u][j], m);
+    k.s = lanes_sum<64>(k.s);
+    k.u = lanes_sum<64>(k.u);
+    const float bound = a.top ? reached_by(best, a.top) : 0.f;
+    if (tid == 0) s_count = 0;
+    if (lane == 0) {
+        s_sums[wave] = k;
+        s_bound[wave] = bound;
+    }
+    __syncthreads();
+    k = joined(joined(s_sums[0], s_sums[1]), joined(s_sums[2], s_sums[3]));
+    k.m = p.parts == 1 ? centre(k.m) : k.m;
+    const float log_s = logf(k.s);
+    if (tid == 0) {
+        if (p.parts == 1) store_sums(a, row, target_score, k, log_s);
+        else *(Sums *)((char *)p.sums + (row * p.parts + part) * SUMS_BYTES) = k;
+    }
+    if (a.top == 0) return;
+    const float least = fmaxf(fmaxf(s_bound[0], s_bound[1]), fmaxf(s_bound[2], s_bound[3]));
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+        if (__any(most[u] >= least && most[u] > -INFINITY)) {
+#pragma unroll
+            for (int j = 0; j < N; ++j)
+                if (v[u][j] >= least && v[u][j] > -INFINITY) {
+                    const int i = atomicAdd(&s_count, 1);
+                    if (i < PART_LIST) {
+                        s_value[i] = v[u][j];
+                        s_from[i] = c0 + u * 256 * N + j;
+                    }
+                }
         }
-        last = best;
-        last_c = best_c;
+    __syncthreads();
+    const int found = s_count;
+    auto put = [&](int i, float value, int c) {
+        if (p.parts == 1) store_top(a, row * a.top + i, value, c, k, log_s);
+        else p.best[(row * p.parts + part) * a.top + i] = make_float2(value, __builtin_bit_cast(float, c));
+    };
+    if (found <= PART_LIST) {
+        for (int i = tid; i < found; i += 256) {
+            const float value = s_value[i];
+            const int c = s_from[i];
+            int rank = 0;
+            for (int o = 0; o < found; ++o) rank += s_value[o] > value || (s_value[o] == value && s_from[o] < c);
+            if (rank < a.top) put(rank, value, c);
+        }
+        for (int i = found + tid; i < a.top; i += 256) put(i, -INFINITY, NO_CLASS);
+        return;
+    }
+    for (int i = 0; i < a.top; ++i) {
+        best = -INFINITY;
+        int c = NO_CLASS;
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int j = 0; j < N; ++j) best = fmaxf(best, v[u][j]);
+        best = lanes_max<64>(best);
+#pragma unroll
+        for (int u = U - 1; u >= 0; --u)
+#pragma unroll
+            for (int j = N - 1; j >= 0; --j)
+                if (v[u][j] == best) c = c0 + u * 256 * N + j;
+        c = lanes_min<64>(c);
         if (lane == 0) {
-            a.top_logp[top_at + k * top_step] = best == -INFINITY ? -INFINITY : best - m - log_s;
-            a.top_class[top_at + k * top_step] = best == -INFINITY ? -1 : best_c;
+            s_best[wave] = best;
+            s_class[wave] = c;
+        }
+        __syncthreads();
+        best = s_best[0];
+        c = s_class[0];
+        for (int w = 1; w < 4; ++w)
+            if (s_best[w] > best || (s_best[w] == best && s_class[w] < c)) {
+                best = s_best[w];
+                c = s_class[w];
+            }
+        __syncthreads();
+        if (tid == 0) put(i, best, c);
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int j = 0; j < N; ++j)
+                if (c0 + u * 256 * N + j == c) v[u][j] = -INFINITY;
+    }
+}
+
+// The parts of a row, one to a lane of the row's wave: sums joined, lists (each in order) merged by their heads.
+constexpr int PARTS_MAX = 64;
+template <class T>
+__global__ __launch_bounds__(64) void logp_join_kernel(const T *__restrict__ x, LogpArgs a, LogpParts p)
+{
+    extern __shared__ float2 s_lists[];          // [parts][top]
+    const int lane = threadIdx.x;
+    const int64_t row = blockIdx.x;
+    const int t = a.target ? a.target[row] : 0;
+    if (ignored(a, t)) return;
+    const float target_score = lane == 0 && a.target ? to_f32(x[row / a.N * a.bs + row % a.N * a.ps + t]) : 0.f;
+    Sums k = lane < p.parts ? *(const Sums *)((const char *)p.sums + (row * p.parts + lane) * SUMS_BYTES) : Sums{-INFINITY, 0.f, 0.f};
+    const float2 *lists = p.best + row * p.parts * a.top;
+    for (int i = lane; i < p.parts * a.top; i += 64) s_lists[i] = lists[i];
+    const Sums all{lanes_max<64>(k.m), 0.f, 0.f};
+    k = joined(k, all);
+    k.s = lanes_sum<64>(k.s);
+    k.u = lanes_sum<64>(k.u);
+    k.m = centre(k.m);
+    const float log_s = logf(k.s);
+    if (lane == 0) store_sums(a, row, target_score, k, log_s);
+    if (a.top == 0) return;
+    __syncthreads();
+    int at = lane * a.top, end = lane < p.parts ? at + a.top : at;
+    float2 head = at < end ? s_lists[at] : make_float2(-INFINITY, __builtin_bit_cast(float, NO_CLASS));
+    for (int i = 0; i < a.top; ++i) {
+        const float best = lanes_max<64>(head.x);
+        const int own = __builtin_bit_cast(int, head.y);
+        const int c = lanes_min<64>(head.x == best ? own : NO_CLASS);
+        if (lane == 0) store_top(a, row * a.top + i, best, c, k, log_s);
+        if (own == c && head.x == best) {
+            ++at;
+            head = at < end ? s_lists[at] : make_float2(-INFINITY, __builtin_bit_cast(float, NO_CLASS));
         }
     }
 }
+
+// ---- channel-major --------------------------------------------------------------------------------------------------------
+// A lane to a position, W waves of a workgroup share the classes: R of them a wave in registers, or (R = 0) any number, read again
+// for each alternative.  What the waves find meets in LDS.
+template <class T, int W, int R>
+__global__ __launch_bounds__(64 * W) void logp_cols_kernel(const T *__restrict__ x, LogpArgs a)
+{
+    __shared__ Sums s_sums[W][64];
+    __shared__ float s_best[W][64];
+    __shared__ int s_class[W][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t tiles = (a.N + 63) / 64, b = blockIdx.x / tiles;
+    const int n = (int)(blockIdx.x % tiles) * 64 + lane;
+    const bool mine = n < a.N;
+    const int64_t row = b * a.N + n;
+    const int t = mine && a.target ? a.target[row] : 0;
+    const bool skip = !mine || ignored(a, t);
+    const T *at = x + b * a.bs + n;
+    const int per = R ? R : (a.C + W - 1) / W, first = wave * per, last = min(first + per, a.C);
+    float v[R ? R : 1];
+    Sums k{-INFINITY, 0.f, 0.f};
+    float best = -INFINITY;
+    if (R) {
+#pragma unroll
+        for (int i = 0; i < R; ++i) v[i] = !skip && first + i < last ? to_f32(at[(first + i) * a.cs]) : -INFINITY;
+#pragma unroll
+        for (int i = 0; i < R; ++i) best = fmaxf(best, v[i]);
+        k.m = best;
+        const float m = centre(best);
+#pragma unroll
+        for (int i = 0; i < R; ++i) add_score(k, v[i], m);
+    } else if (!skip) {
+        for (int c = first; c < last; ++c) best = fmaxf(best, to_f32(at[c * a.cs]));
+        k.m = best;
+        const float m = centre(best);
+        for (int c = first; c < last; ++c) add_score(k, to_f32(at[c * a.cs]), m);
+    }
+    if (W > 1) {
+        s_sums[wave][lane] = k;
+        __syncthreads();
+        k = s_sums[0][lane];
+#pragma unroll
+        for (int w = 1; w < W; ++w) k = joined(k, s_sums[w][lane]);
+    }
+    k.m = centre(k.m);
+    const float log_s = logf(k.s);
+    if (wave == 0 && mine) {
+        if (skip) a.logp[row] = a.entropy[row] = a.lse[row] = 0.f;
+        else store_sums(a, row, a.target ? to_f32(at[t * a.cs]) : 0.f, k, log_s);
+    }
+    float last_best = INFINITY;
+    int last_class = -1;
+    for (int i = 0; i < a.top; ++i) {
+        best = -INFINITY;
+        int c = NO_CLASS;
+        if (R) {
+#pragma unroll
+            for (int r = 0; r < R; ++r)
+                if (v[r] > best) { best = v[r]; c = first + r; }
+        } else if (!skip) {
+            for (int r = first; r < last; ++r) {
+                const float y = to_f32(at[r * a.cs]);
+                if (y > best && (y < last_best || (y == last_best && r > last_class))) { best = y; c = r; }
+            }
+        }
+        if (W > 1) {
+            s_best[wave][lane] = best;
+            s_class[wave][lane] = c;
+            __syncthreads();
+            best = s_best[0][lane];
+            c = s_class[0][lane];
+#pragma unroll
+            for (int w = 1; w < W; ++w)
+                if (s_best[w][lane] > best) { best = s_best[w][lane]; c = s_class[w][lane]; }
+            __syncthreads();
+        }
+        if (wave == 0 && mine) store_top(a, (b * a.top + i) * a.N + n, best, c, k, log_s);
+        last_best = best;
+        last_class = c;
+        if (R)
+#pragma unroll
+            for (int r = 0; r < R; ++r)
+                if (first + r == c) v[r] = -INFINITY;
+    }
+}
+
+// ---- gradient -------------------------------------------------------------------------------------------------------------
 
 struct LogpBwdArgs {
     const int32_t *target;
@@ -84,29 +419,169 @@ struct LogpBwdArgs {
     int64_t rows, bs, ps, cs, gbs, gps, gcs;     // strides of the scores and of their gradient
     int N, C;
 };
+struct LogpBwdRow {
+    int t;
+    bool zero;
+    float lse, gl, gh, h;
+    __device__ __forceinline__ LogpBwdRow(const LogpBwdArgs &a, int64_t row)
+    {
+        t = a.target ? a.target[row] : -1;
+        lse = a.lse[row];
+        zero = (a.target && (t < 0 || t >= a.C)) || lse == -INFINITY;
+        gl = a.grad_logp ? a.grad_logp[row] : 0.f;
+        gh = a.grad_entropy ? a.grad_entropy[row] : 0.f;
+        h = a.grad_entropy ? a.entropy[row] : 0.f;
+    }
+    __device__ __forceinline__ float operator()(float x, int c) const
+    {
+        const float lp = x - lse, p = __builtin_amdgcn_exp2f(lp * LOG2E);
+        const float v = -p * (gl + gh * (fmaxf(lp, MASKED) + h));
+        return c == t ? v + gl : v;
+    }
+};
 
-template <class T>
-__global__ __launch_bounds__(256) void logp_bwd_kernel(const T *x, T *gx, LogpBwdArgs a)
+// Point-major: L lanes to a row, U times 16 bytes each, `chunks` workgroups behind one another along long rows (L = 256).
+template <class T, int L, int U>
+__global__ __launch_bounds__(256) void logp_bwd_rows_kernel(const T *x, T *gx, LogpBwdArgs a, int chunks)
 {
-    const int lane = threadIdx.x & 63;
-    const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    constexpr int N = LANE_ELEMENTS<T>;
+    const int64_t row = L == 256 ? blockIdx.x / chunks : (int64_t)blockIdx.x * (256 / L) + threadIdx.x / L;
     if (row >= a.rows) return;
     const int64_t b = row / a.N, n = row % a.N;
     const T *at = x + b * a.bs + n * a.ps;
     T *to = gx + b * a.gbs + n * a.gps;
-    const int t = a.target ? a.target[row] : -1;
-    const float lse = a.lse[row];
-    if ((a.target && (t < 0 || t >= a.C)) || lse == -INFINITY) {
-        for (int c = lane; c < a.C; c += 64) to[c * a.gcs] = (T)0.f;
-        return;
+    const int c0 = ((L == 256 ? (int)(blockIdx.x % chunks) * U * L : 0) + (int)(threadIdx.x % L)) * N;
+    const LogpBwdRow f(a, row);
+    float v[U][N];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        if (f.zero) {
+#pragma unroll
+            for (int j = 0; j < N; ++j) v[u][j] = 0.f;
+        } else
+            Chunk<T>::load_row(at, c0 + u * L * N, a.C, v[u], 0.f);
     }
-    const float gl = a.target && a.grad_logp ? a.grad_logp[row] : 0.f, gh = a.grad_entropy ? a.grad_entropy[row] : 0.f;
-    const float h = a.grad_entropy ? a.entropy[row] : 0.f;
-    for (int c = lane; c < a.C; c += 64) {
-        const float lp = to_f32(at[c * a.cs]) - lse, p = __builtin_amdgcn_exp2f(lp * LOG2E);
-        const float v = -p * (gl + gh * (fmaxf(lp, MASKED) + h));
-        to[c * a.gcs] = (T)(c == t ? v + gl : v);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        if (!f.zero)
+#pragma unroll
+            for (int j = 0; j < N; ++j) v[u][j] = f(v[u][j], c0 + u * L * N + j);
+        Chunk<T>::store_row(to, c0 + u * L * N, a.C, v[u]);
     }
+}
+
+// Channel-major: a lane to a position, a workgroup to 256 of them and 16 classes.
+constexpr int BWD_CLASSES = 16;
+template <class T>
+__global__ __launch_bounds__(256) void logp_bwd_cols_kernel(const T *x, T *gx, LogpBwdArgs a, int tiles, int parts)
+{
+    const int part = blockIdx.x % parts, tile = blockIdx.x / parts % tiles;
+    const int64_t b = blockIdx.x / parts / tiles;
+    const int n = tile * 256 + threadIdx.x;
+    if (n >= a.N) return;
+    const int first = part * BWD_CLASSES, many = min(BWD_CLASSES, a.C - first);
+    const T *at = x + b * a.bs + first * a.cs + n;
+    T *to = gx + b * a.gbs + first * a.gcs + n;
+    const LogpBwdRow f(a, b * a.N + n);
+    float v[BWD_CLASSES];
+#pragma unroll
+    for (int i = 0; i < BWD_CLASSES; ++i)
+        if (i < many && !f.zero) v[i] = to_f32(at[i * a.cs]);
+#pragma unroll
+    for (int i = 0; i < BWD_CLASSES; ++i)
+        if (i < many) to[i * a.gcs] = (T)(f.zero ? 0.f : f(v[i], first + i));
+}
+
+// ---- launches -------------------------------------------------------------------------------------------------------------
+
+// Columns that a row kernel of (L, U) holds; the smallest that holds C is taken.
+template <class T, class F>
+static hipError_t with_row_lanes(int C, F f)
+{
+    constexpr int N = LANE_ELEMENTS<T>;
+    if (C <= 4 * N) return f(std::integral_constant<int, 4>{}, std::integral_constant<int, 1>{});
+    if (C <= 8 * N) return f(std::integral_constant<int, 8>{}, std::integral_constant<int, 1>{});
+    if (C <= 16 * N) return f(std::integral_constant<int, 16>{}, std::integral_constant<int, 1>{});
+    if (C <= 32 * N) return f(std::integral_constant<int, 32>{}, std::integral_constant<int, 1>{});
+    if (C <= 64 * N) return f(std::integral_constant<int, 64>{}, std::integral_constant<int, 1>{});
+    return f(std::integral_constant<int, 64>{}, std::integral_constant<int, 2>{});
+}
+static int row_columns_max(int dtype) { return 2048 / (int)dtype_bytes(dtype); }      // 64 lanes x 2 x 16 bytes
+
+// How a long row is cut: 16-byte pieces a thread takes (2, 4 or 8, fp32 16), the longest with which there are two workgroups to a
+// compute unit, and enough that a row has at most PARTS_MAX parts.
+struct PartPlan {
+    int U, parts;
+};
+static PartPlan plan_parts(int64_t rows, int C, int dtype)
+{
+    const int lane = 16 / (int)dtype_bytes(dtype);
+    PartPlan p{};
+    for (p.U = 16; ; p.U /= 2) {
+        p.parts = (int)cdiv64(C, 256 * lane * p.U);
+        if (p.U == 2 || (rows * p.parts >= 2 * device_cu_count() && (dtype == FLEX_F32 || p.U < 16))) break;
+    }
+    while (p.parts > PARTS_MAX) {
+        p.U *= 2;
+        p.parts = (int)cdiv64(C, 256 * lane * p.U);
+    }
+    return p;
+}
+static size_t parts_sums_bytes(int64_t rows, int parts) { return align256((size_t)rows * parts * SUMS_BYTES); }
+
+template <class T>
+static hipError_t launch_logp_rows(const T *x, const LogpArgs &a, int dtype, void *ws, hipStream_t s)
+{
+    if (a.C <= row_columns_max(dtype))
+        return with_row_lanes<T>(a.C, [&](auto l, auto u) {
+            constexpr int L = decltype(l)::value, U = decltype(u)::value;
+            hipLaunchKernelGGL((logp_rows_kernel<T, L, U>), dim3((unsigned)cdiv64(a.rows, 256 / L)), dim3(256), 0, s, x, a);
+            return hipGetLastError();
+        });
+    const PartPlan q = plan_parts(a.rows, a.C, dtype);
+    const LogpParts p{(Sums *)ws, (float2 *)((char *)ws + parts_sums_bytes(a.rows, q.parts)), q.parts};
+    const dim3 grid((unsigned)(a.rows * q.parts)), wg(256);
+    if (q.U == 2) hipLaunchKernelGGL((logp_part_kernel<T, 2>), grid, wg, 0, s, x, a, p);
+    else if (q.U == 4) hipLaunchKernelGGL((logp_part_kernel<T, 4>), grid, wg, 0, s, x, a, p);
+    else if (q.U == 8) hipLaunchKernelGGL((logp_part_kernel<T, 8>), grid, wg, 0, s, x, a, p);
+    else if constexpr (sizeof(T) == 4) hipLaunchKernelGGL((logp_part_kernel<T, 16>), grid, wg, 0, s, x, a, p);
+    if (q.parts > 1)
+        hipLaunchKernelGGL(logp_join_kernel<T>, dim3((unsigned)a.rows), dim3(64), sizeof(float2) * q.parts * a.top, s, x, a, p);
+    return hipGetLastError();
+}
+
+template <class T>
+static hipError_t launch_logp_cols(const T *x, const LogpArgs &a, int B, hipStream_t s)
+{
+    const dim3 grid((unsigned)(B * cdiv64(a.N, 64)));
+    if (a.C <= 16) hipLaunchKernelGGL((logp_cols_kernel<T, 1, 16>), grid, dim3(64), 0, s, x, a);
+    else if (a.C <= 32) hipLaunchKernelGGL((logp_cols_kernel<T, 2, 16>), grid, dim3(128), 0, s, x, a);
+    else if (a.C <= 64) hipLaunchKernelGGL((logp_cols_kernel<T, 4, 16>), grid, dim3(256), 0, s, x, a);
+    else if (a.C <= 128) hipLaunchKernelGGL((logp_cols_kernel<T, 8, 16>), grid, dim3(512), 0, s, x, a);
+    else hipLaunchKernelGGL((logp_cols_kernel<T, 16, 0>), grid, dim3(1024), 0, s, x, a);
+    return hipGetLastError();
+}
+
+template <class T>
+static hipError_t launch_logp_bwd(const T *x, T *gx, const LogpBwdArgs &a, int B, bool bcn, int dtype, hipStream_t s)
+{
+    if (bcn) {
+        const int tiles = (a.N + 255) / 256, parts = (a.C + BWD_CLASSES - 1) / BWD_CLASSES;
+        const int64_t grid = (int64_t)B * tiles * parts;
+        if (grid >= ((int64_t)1 << 31)) return hipErrorInvalidValue;
+        hipLaunchKernelGGL(logp_bwd_cols_kernel<T>, dim3((unsigned)grid), dim3(256), 0, s, x, gx, a, tiles, parts);
+        return hipGetLastError();
+    }
+    if (a.C <= row_columns_max(dtype))
+        return with_row_lanes<T>(a.C, [&](auto l, auto u) {
+            constexpr int L = decltype(l)::value, U = decltype(u)::value;
+            hipLaunchKernelGGL((logp_bwd_rows_kernel<T, L, U>), dim3((unsigned)cdiv64(a.rows, 256 / L)), dim3(256), 0, s, x, gx, a, 1);
+            return hipGetLastError();
+        });
+    constexpr int U = 2;
+    const int chunks = (int)cdiv64(a.C, 256 * LANE_ELEMENTS<T> * U);
+    hipLaunchKernelGGL((logp_bwd_rows_kernel<T, 256, U>), dim3((unsigned)(a.rows * chunks)), dim3(256), 0, s, x, gx, a, chunks);
+    return hipGetLastError();
 }
 
 }  // namespace flex
@@ -117,7 +592,9 @@ static bool logp_sizes_ok(int B, int N, int C, int64_t row_stride, int dtype, in
 {
     return B > 0 && N > 0 && C > 0 && C <= FLEX_LOGP_MAX_CLASSES && (int64_t)B * N < ((int64_t)1 << 31) &&
            (layout == FLEX_LAYOUT_BCN || layout == FLEX_LAYOUT_BNC) && dtype_ok(dtype) &&
-           row_stride >= (layout == FLEX_LAYOUT_BCN ? N : C) && row_stride < ((int64_t)1 << 31);
+           row_stride >= (layout == FLEX_LAYOUT_BCN ? N : C) && row_stride < ((int64_t)1 << 31) &&
+           // workgroups of 4 KB of a row, or of 256 positions and 16 classes
+           (layout == FLEX_LAYOUT_BCN ? cdiv64(N, 256) * B * cdiv64(C, 16) : (int64_t)B * N * cdiv64(C, 1024)) < ((int64_t)1 << 31);
 }
 
 extern "C" {
@@ -125,7 +602,10 @@ extern "C" {
 size_t flexlogp_fwd_workspace_bytes(int B, int N, int C, int top, int dtype, int layout)
 {
     if (!logp_sizes_ok(B, N, C, layout == FLEX_LAYOUT_BCN ? N : C, dtype, layout) || top < 0 || top > FLEX_LOGP_MAX_TOP || top > C) return 0;
-    return 256;
+    if (layout == FLEX_LAYOUT_BCN || C <= row_columns_max(dtype)) return 256;
+    const int64_t rows = (int64_t)B * N;
+    const int parts = plan_parts(rows, C, dtype).parts;
+    return parts == 1 ? 256 : parts_sums_bytes(rows, parts) + align256((size_t)rows * parts * top * sizeof(float2));
 }
 
 int flexlogp_fwd(const void *logits, const int32_t *target, float *logp, float *entropy, float *lse, float *top_logp,
@@ -138,12 +618,12 @@ int flexlogp_fwd(const void *logits, const int32_t *target, float *logp, float *
     if (!workspace || ((uintptr_t)workspace & 255) || workspace_bytes < flexlogp_fwd_workspace_bytes(B, N, C, top, dtype, layout))
         return FLEX_ERR_WORKSPACE;
     const bool bcn = layout == FLEX_LAYOUT_BCN;
-    LogpArgs a{target, logp, entropy, lse, top_logp, top_class, (int64_t)B * N, (bcn ? C : N) * row_stride,
-               bcn ? 1 : row_stride, bcn ? row_stride : 1, N, C, top, bcn};
+    const LogpArgs a{target, logp, entropy, lse, top_logp, top_class, (int64_t)B * N, (bcn ? C : N) * row_stride,
+                     bcn ? 1 : row_stride, bcn ? row_stride : 1, N, C, top};
     const hipError_t e = with_dtype(dtype, [&](auto t) {
         typedef decltype(t) T;
-        hipLaunchKernelGGL(logp_fwd_kernel<T>, dim3((unsigned)cdiv64(a.rows, 4)), dim3(256), 0, (hipStream_t)stream, (const T *)logits, a);
-        return hipGetLastError();
+        return bcn ? launch_logp_cols<T>((const T *)logits, a, B, (hipStream_t)stream)
+                   : launch_logp_rows<T>((const T *)logits, a, dtype, workspace, (hipStream_t)stream);
     });
     return e == hipSuccess ? FLEX_OK : FLEX_ERR_HIP;
 }
@@ -157,14 +637,12 @@ int flexlogp_bwd(const void *logits, const int32_t *target, const float *lse, co
     if (!logp_sizes_ok(B, N, C, row_stride, dtype, layout) || !logp_sizes_ok(B, N, C, grad_row_stride, dtype, layout)) return FLEX_ERR_SHAPE;
     if (logits == grad_logits && row_stride != grad_row_stride) return FLEX_ERR_SHAPE;
     const bool bcn = layout == FLEX_LAYOUT_BCN;
-    LogpBwdArgs a{target, lse, entropy, grad_logp, grad_entropy, (int64_t)B * N,
-                  (bcn ? C : N) * row_stride, bcn ? 1 : row_stride, bcn ? row_stride : 1,
-                  (bcn ? C : N) * grad_row_stride, bcn ? 1 : grad_row_stride, bcn ? grad_row_stride : 1, N, C};
+    const LogpBwdArgs a{target, lse, entropy, grad_logp, grad_entropy, (int64_t)B * N,
+                        (bcn ? C : N) * row_stride, bcn ? 1 : row_stride, bcn ? row_stride : 1,
+                        (bcn ? C : N) * grad_row_stride, bcn ? 1 : grad_row_stride, bcn ? grad_row_stride : 1, N, C};
     const hipError_t e = with_dtype(dtype, [&](auto t) {
         typedef decltype(t) T;
-        hipLaunchKernelGGL(logp_bwd_kernel<T>, dim3((unsigned)cdiv64(a.rows, 4)), dim3(256), 0, (hipStream_t)stream, (const T *)logits,
-                           (T *)grad_logits, a);
-        return hipGetLastError();
+        return launch_logp_bwd<T>((const T *)logits, (T *)grad_logits, a, B, bcn, dtype, (hipStream_t)stream);
     });
     return e == hipSuccess ? FLEX_OK : FLEX_ERR_HIP;
 }
