@@ -3,6 +3,7 @@
 #pragma once
 #include "flex_common.hpp"
 #include "../../include/flexconv.h"
+#include <type_traits>
 
 namespace flex {
 
@@ -42,13 +43,15 @@ struct Chunk {
         for (int j = 0; j < N; ++j) v[j] = (T)x[j];
         *(V *)p = v;
     }
-    // columns c0 .. of a row of C, `fill` behind its end
-    static __device__ __forceinline__ void load_row(const T *row, int c0, int C, float (&x)[N], float fill)
+    // Where a lane that is to take columns c0 .. of a row of C >= N reads: at the row's last N columns rather than past its end, so
+    // that no load waits in a branch.  What is not its own then (before c0) is for mask() to overwrite.
+    static __device__ __forceinline__ int from(int c0, int C) { return min(c0, C - N); }
+    static __device__ __forceinline__ void mask(float (&x)[N], int c0, int C, float fill)
     {
-        if (c0 + N <= C) load(row + c0, x);
-        else
+        if (c0 + N > C)
 #pragma unroll
-            for (int j = 0; j < N; ++j) x[j] = c0 + j < C ? to_f32(row[c0 + j]) : fill;
+            for (int j = 0; j < N; ++j)
+                if (C - N + j < c0) x[j] = fill;
     }
     static __device__ __forceinline__ void store_row(T *row, int c0, int C, const float (&x)[N])
     {
@@ -61,28 +64,34 @@ struct Chunk {
 };
 
 // ---- reductions over groups of L neighbouring lanes, the result on every one of them -----------------------------------------
-// Up to 16 lanes by DPP (quad permutes, then the mirrored half row and row, whose halves hold one value each by then); all lanes of
-// a group have to be active.
-
-template <int CTRL>
-__device__ __forceinline__ float dpp_f32(float v)
-{
-    return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CTRL, 0xF, 0xF, true));
-}
-template <int CTRL>
-__device__ __forceinline__ int dpp_i32(int v) { return __builtin_amdgcn_update_dpp(0, v, CTRL, 0xF, 0xF, true); }
+// Up to 16 lanes by DPP (quad permutes, then the mirrored half row and row, whose halves hold one value each by then), then by
+// swapping rows of 16 and halves of 32 lanes between a value and its copy; all lanes of a group have to be active.
 
 constexpr int DPP_XOR1 = 0xB1, DPP_XOR2 = 0x4E, DPP_HALF_MIRROR = 0x141, DPP_MIRROR = 0x140;
 
-template <int L, class Op>
-__device__ __forceinline__ float lanes_reduce(float v, Op op)
+// op of the two values that swap(v, v) leaves.  They pass through an empty statement: the compiler takes them for one value otherwise
+// where op is a maximum, and leaves that out.
+template <class V, class Swap, class Op>
+__device__ __forceinline__ V swap_reduce(V v, Swap swap, Op op)
 {
-    if (L >= 2) v = op(v, dpp_f32<DPP_XOR1>(v));
-    if (L >= 4) v = op(v, dpp_f32<DPP_XOR2>(v));
-    if (L >= 8) v = op(v, dpp_f32<DPP_HALF_MIRROR>(v));
-    if (L >= 16) v = op(v, dpp_f32<DPP_MIRROR>(v));
-    if (L >= 32) v = op(v, __shfl_xor(v, 16));
-    if (L >= 64) v = op(v, __shfl_xor(v, 32));
+    const unsigned b = __builtin_bit_cast(unsigned, v);
+    const auto r = swap(b, b);
+    unsigned one = r[0], two = r[1];
+    asm("" : "+v"(one), "+v"(two));
+    return op(__builtin_bit_cast(V, one), __builtin_bit_cast(V, two));
+}
+template <int L, class V, class Op>
+__device__ __forceinline__ V lanes_reduce(V v, Op op)
+{
+    const auto moved = [](V v, auto ctrl) {
+        return __builtin_bit_cast(V, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), decltype(ctrl)::value, 0xF, 0xF, true));
+    };
+    if (L >= 2) v = op(v, moved(v, std::integral_constant<int, DPP_XOR1>{}));
+    if (L >= 4) v = op(v, moved(v, std::integral_constant<int, DPP_XOR2>{}));
+    if (L >= 8) v = op(v, moved(v, std::integral_constant<int, DPP_HALF_MIRROR>{}));
+    if (L >= 16) v = op(v, moved(v, std::integral_constant<int, DPP_MIRROR>{}));
+    if (L >= 32) v = swap_reduce(v, [](unsigned a, unsigned b) { return __builtin_amdgcn_permlane16_swap(a, b, false, false); }, op);
+    if (L >= 64) v = swap_reduce(v, [](unsigned a, unsigned b) { return __builtin_amdgcn_permlane32_swap(a, b, false, false); }, op);
     return v;
 }
 template <int L>
@@ -98,13 +107,7 @@ __device__ __forceinline__ float lanes_max(float v)
 template <int L>
 __device__ __forceinline__ int lanes_min(int v)
 {
-    if (L >= 2) v = min(v, dpp_i32<DPP_XOR1>(v));
-    if (L >= 4) v = min(v, dpp_i32<DPP_XOR2>(v));
-    if (L >= 8) v = min(v, dpp_i32<DPP_HALF_MIRROR>(v));
-    if (L >= 16) v = min(v, dpp_i32<DPP_MIRROR>(v));
-    if (L >= 32) v = min(v, __shfl_xor(v, 16));
-    if (L >= 64) v = min(v, __shfl_xor(v, 32));
-    return v;
+    return lanes_reduce<L>(v, [](int a, int b) { return min(a, b); });
 }
 
 // a vector over the channels in a parameter type that is known at run time (read rarely: once a workgroup, or from a cache)

@@ -12,7 +12,7 @@
 
 namespace flex {
 
-constexpr float LOG2E = 1.4426950408889634f;
+constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 constexpr float MASKED = -1e5f;       // stands for x - m = -inf where it is multiplied by exp(x - m) = 0
 constexpr int NO_CLASS = 0x7FFFFFFF;
 
@@ -20,7 +20,7 @@ struct LogpArgs {
     const int32_t *target;
     float *logp, *entropy, *lse, *top_logp;
     int32_t *top_class;
-    int64_t rows, bs, ps, cs;         // positions; element strides: cloud, position, class
+    int64_t rows, stride;             // positions; elements from row to row: of a position's scores, or of a class's (channel-major)
     int N, C, top;
 };
 
@@ -61,7 +61,8 @@ __device__ __forceinline__ bool ignored(const LogpArgs &a, int t) { return a.tar
 // ---- point-major, rows of up to 64 lanes' elements ------------------------------------------------------------------------
 // L lanes hold a row, U times 16 bytes each.  The best score is the maximum over the lanes, its class the smallest among those that
 // hold it; it is then taken out, and so on for each alternative: 2 log2 L steps and three operations an element each.
-template <class T, int L, int U>
+// NARROW: rows of fewer classes than 16 bytes hold.
+template <class T, int L, int U, bool NARROW>
 __global__ __launch_bounds__(256) void logp_rows_kernel(const T *__restrict__ x, LogpArgs a)
 {
     constexpr int N = LANE_ELEMENTS<T>;
@@ -70,16 +71,26 @@ __global__ __launch_bounds__(256) void logp_rows_kernel(const T *__restrict__ x,
     const bool mine = row < a.rows;
     const int t = mine && a.target ? a.target[row] : 0;
     const bool skip = !mine || ignored(a, t);
-    const T *at = x + row / a.N * a.bs + row % a.N * a.ps;
+    const T *at = x + row * a.stride;
     float v[U][N];
+    int from[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-        if (skip)
+        const int c0 = (u * L + sub) * N;
+        from[u] = NARROW ? c0 : Chunk<T>::from(c0, a.C);
 #pragma unroll
-            for (int j = 0; j < N; ++j) v[u][j] = -INFINITY;
-        else
-            Chunk<T>::load_row(at, (u * L + sub) * N, a.C, v[u], -INFINITY);
+        for (int j = 0; j < N; ++j) v[u][j] = -INFINITY;
+        if (skip) continue;
+        if (NARROW) {
+#pragma unroll
+            for (int j = 0; j < N; ++j)
+                if (c0 + j < a.C) v[u][j] = to_f32(at[c0 + j]);
+        } else
+            Chunk<T>::load(at + from[u], v[u]);
     }
+    if (!NARROW)
+#pragma unroll
+        for (int u = 0; u < U; ++u) Chunk<T>::mask(v[u], (u * L + sub) * N, a.C, -INFINITY);
     const float target_score = !skip && sub == 0 && a.target ? to_f32(at[t]) : 0.f;
     float best = -INFINITY;
 #pragma unroll
@@ -107,7 +118,7 @@ __global__ __launch_bounds__(256) void logp_rows_kernel(const T *__restrict__ x,
         for (int u = U - 1; u >= 0; --u)
 #pragma unroll
             for (int j = N - 1; j >= 0; --j)
-                if (v[u][j] == best) c = (u * L + sub) * N + j;
+                if (v[u][j] == best) c = from[u] + j;
         c = lanes_min<L>(c);
         if (mine && sub == i % L) store_top(a, row * a.top + i, best, c, k, log_s);
         if (i + 1 == a.top) break;
@@ -116,7 +127,7 @@ __global__ __launch_bounds__(256) void logp_rows_kernel(const T *__restrict__ x,
         for (int u = 0; u < U; ++u)
 #pragma unroll
             for (int j = 0; j < N; ++j) {
-                if ((u * L + sub) * N + j == c) v[u][j] = -INFINITY;
+                if (from[u] + j == c) v[u][j] = -INFINITY;
                 best = fmaxf(best, v[u][j]);
             }
         best = lanes_max<L>(best);
@@ -124,11 +135,15 @@ __global__ __launch_bounds__(256) void logp_rows_kernel(const T *__restrict__ x,
 }
 
 // ---- point-major, longer rows ---------------------------------------------------------------------------------------------
-// A workgroup holds a part of a row, 256 x U x 16 bytes, in registers.  Alternatives: the `top`-th largest of a wave's 64 lane maxima
-// bounds the part's `top`-th largest score from below, and so does the largest of the four waves' bounds; what reaches it,
-// little more than `top` scores in most rows, goes to a list in LDS and is ranked there.  A list that overflows (rows full of equal
-// scores) is left for `top` rounds over the registers.  Parts of one row meet in logp_join_kernel.
-constexpr int PART_LIST = 512;
+// A workgroup runs along a part of a row, 16 KB at a time, the next 16 KB on their way meanwhile.  A lane's sums are about its own
+// maximum so far and meet at the end.  What an element costs decides beside the memory (bf16: 2 bytes in the time of some 11 vector
+// operations): exp counts four, the product and difference in front of it are one fused operation, the maximum takes two elements a
+// step.
+// Alternatives: the `top`-th largest of a wave's 64 lane maxima so far is reached by `top` of its scores, so only what reaches it
+// can be among the best; that goes to the wave's list in LDS, some two `top`s in most rows.  A list that fills up (rows of equal
+// scores, ascending rows) is cut to the best `top`, after which, since a wave meets its classes in ascending order (but for the two
+// halves of 16-bit pieces), later scores have to exceed the last of them.  The lists meet in one, cut by the largest bound of the four waves, and are ranked there.  Parts
+// of one row meet in logp_join_kernel.
 
 // the bits of a float, ordered like the floats
 __device__ __forceinline__ uint32_t order_key(float v)
@@ -154,21 +169,58 @@ __device__ __forceinline__ float reached_by(float v, int n)
     return found <= order_key(-INFINITY) ? -INFINITY : from_order_key(found);
 }
 
+// Candidates for the alternatives in LDS, score and class (as bits).  f(place, score, class) for each of them, its place the number of
+// those before it, by `threads` threads; seven entries behind the list are read, and have to be there.
+template <class F>
+__device__ __forceinline__ void each_ranked(const float2 *list, int found, int tid, int threads, F f)
+{
+    for (int i = tid; i < found; i += threads) {
+        const float value = list[i].x;
+        const int c = __builtin_bit_cast(int, list[i].y);
+        int rank = 0;
+        for (int o = 0; o < found; o += 8)
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                const float2 e = list[o + k];
+                rank += o + k < found && (e.x > value || (e.x == value && __builtin_bit_cast(int, e.y) < c));
+            }
+        f(rank, value, c);
+    }
+}
+
 // What a part leaves of itself: its sums and its best scores with their classes.
 struct LogpParts {
     Sums *sums;                       // [rows][parts], 16 bytes apart
     float2 *best;                     // [rows][parts][top]: score, class (as bits)
-    int parts;
+    int parts, spans;                 // parts of a row, spans of a part
 };
-constexpr int SUMS_BYTES = 16;
+constexpr int SUMS_BYTES = 16, SPAN_LOADS = 4;
+template <class T>
+constexpr int SPAN = 256 * LANE_ELEMENTS<T> * SPAN_LOADS;     // elements that a workgroup takes at a time: 16 KB
 
-template <class T, int U>
+constexpr float LOWEST = -3.4028234663852886e38f, HUGE_SCORE = 1e37f;
+constexpr int WAVE_LIST = 64 * 4 + FLEX_LOGP_MAX_TOP, LISTS_JOINED = 512;
+
+__device__ __forceinline__ float max3(float a, float b, float c)
+{
+    float r;
+    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+    return r;
+}
+__device__ __forceinline__ void lds_in_order()
+{
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+}
+
+template <class T>
 __global__ __launch_bounds__(256) void logp_part_kernel(const T *__restrict__ x, LogpArgs a, LogpParts p)
 {
-    constexpr int N = LANE_ELEMENTS<T>;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    constexpr int N = LANE_ELEMENTS<T>, U = SPAN_LOADS, GROUPS = U * N / 4;
+    typedef typename Chunk<T>::V V;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const unsigned part = blockIdx.x % p.parts;
     const int64_t row = blockIdx.x / p.parts;
-    const int part = (int)(blockIdx.x % p.parts);
     const int t = a.target ? a.target[row] : 0;
     if (ignored(a, t)) {
         if (part == 0) {
@@ -181,36 +233,134 @@ __global__ __launch_bounds__(256) void logp_part_kernel(const T *__restrict__ x,
         return;
     }
     __shared__ Sums s_sums[4];
-    __shared__ float s_bound[4], s_best[4];
-    __shared__ int s_count, s_class[4];
-    __shared__ float s_value[PART_LIST];
-    __shared__ int s_from[PART_LIST];
-    const T *at = x + row / a.N * a.bs + row % a.N * a.ps;
-    const int c0 = part * (256 * N * U) + tid * N;
-    float v[U][N];
+    __shared__ float s_bound[4];
+    __shared__ int s_count;
+    __shared__ float2 s_list[4][WAVE_LIST + 8], s_cut[4][FLEX_LOGP_MAX_TOP], s_joined[LISTS_JOINED + 8];
+    float2 *const list = s_list[wave];
+    const T *at = x + row * a.stride;
+    const int begin = (int)part * p.spans * SPAN<T>, end = min(a.C, begin + p.spans * SPAN<T>);
+    V next[U];
+    auto request = [&](int c) {
 #pragma unroll
-    for (int u = 0; u < U; ++u) Chunk<T>::load_row(at, c0 + u * 256 * N, a.C, v[u], -INFINITY);
+        for (int u = 0; u < U; ++u) next[u] = *(const V *)(at + Chunk<T>::from(c + (u * 256 + tid) * N, a.C));
+    };
+    request(begin);
     const float target_score = tid == 0 && a.target && p.parts == 1 ? to_f32(at[t]) : 0.f;
-    float most[U], best = -INFINITY;
+    Sums k{-INFINITY, 0.f, 0.f};       // of the lane; u in units of ln 2
+    float least = LOWEST, bound = LOWEST;       // what a candidate reaches; what `top` scores of the wave are known to reach
+    float same = LOWEST;               // the last of a list that was cut, which a score of the piece at hand may equal
+    int count = 0;                     // the wave's list
+
+    // the list's best `top`, in order
+    auto cut = [&]() {
+        lds_in_order();
+        each_ranked(list, count, lane, 64, [&](int rank, float value, int c) {
+            if (rank < a.top) s_cut[wave][rank] = make_float2(value, __builtin_bit_cast(float, c));
+        });
+        lds_in_order();
+        if (count <= a.top) return;
+        if (lane < a.top) list[lane] = s_cut[wave][lane];
+        count = a.top;
+        const float last = s_cut[wave][a.top - 1].x;
+        bound = fmaxf(bound, last);
+        same = fmaxf(least, last);
+        least = fmaxf(least, from_order_key(order_key(last) + 1));
+        lds_in_order();
+    };
+
+    for (int c = begin; c < end; c += SPAN<T>) {
+        float v[U][N];
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-        most[u] = v[u][0];
+        for (int u = 0; u < U; ++u)
 #pragma unroll
-        for (int j = 1; j < N; ++j) most[u] = fmaxf(most[u], v[u][j]);
-        best = fmaxf(best, most[u]);
+            for (int j = 0; j < N; ++j) v[u][j] = to_f32(next[u][j]);
+        if (c + SPAN<T> < end) request(c + SPAN<T>);
+        if (c + SPAN<T> > a.C)
+#pragma unroll
+            for (int u = 0; u < U; ++u) Chunk<T>::mask(v[u], c + (u * 256 + tid) * N, a.C, -INFINITY);
+        float most[GROUPS], span_most = -INFINITY;
+#pragma unroll
+        for (int g = 0; g < GROUPS; ++g) {
+            const float *w = &v[g / (N / 4)][g % (N / 4) * 4];
+            most[g] = max3(max3(w[0], w[1], w[2]), w[3], -INFINITY);
+            span_most = fmaxf(span_most, most[g]);
+        }
+        const float was = k.m;
+        k.m = fmaxf(was, span_most);
+        const float m = centre(k.m);
+        const bool far = __any(fabsf(m) > HUGE_SCORE);       // m log2(e) may be no number of fp32: the difference first
+        {
+            const float d = fmaxf((was - m) * LOG2E, MASKED), e = __builtin_amdgcn_exp2f(d);
+            k.u = (k.u + k.s * d) * e;
+            k.s *= e;
+        }
+        float s[2] = {0.f, 0.f}, q[2] = {0.f, 0.f};
+        if (!far) {
+            const float shift = m * LOG2E;
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+#pragma unroll
+                for (int j = 0; j < N; ++j) {
+                    const float z = __builtin_fmaf(v[u][j], LOG2E, -shift), e = __builtin_amdgcn_exp2f(z);
+                    s[j & 1] += e;
+                    q[j & 1] = __builtin_fmaf(e, fmaxf(z, MASKED), q[j & 1]);
+                }
+        } else {
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+#pragma unroll
+                for (int j = 0; j < N; ++j) {
+                    const float z = (v[u][j] - m) * LOG2E, e = __builtin_amdgcn_exp2f(z);
+                    s[j & 1] += e;
+                    q[j & 1] = __builtin_fmaf(e, fmaxf(z, MASKED), q[j & 1]);
+                }
+        }
+        k.s += s[0] + s[1];
+        k.u += q[0] + q[1];
+        if (a.top == 0 || !__any(span_most >= least)) continue;
+        bound = fmaxf(bound, reached_by(k.m, a.top));
+        least = fmaxf(least, bound);
+        for (int done = -1;;) {
+            bool full = false;
+#pragma unroll
+            for (int g = 0; g < GROUPS; ++g) {
+                const float reach = g == done && g % (N / 4) ? same : least;
+                if (full || g < done || !__any(most[g] >= reach)) continue;
+                const float *w = &v[g / (N / 4)][g % (N / 4) * 4];
+                uint64_t mask[4];
+                int more = 0;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    mask[j] = __ballot(w[j] >= reach);
+                    more += __popcll(mask[j]);
+                }
+                if (count + more > WAVE_LIST) {
+                    full = true;
+                    done = g;
+                    continue;
+                }
+                const int from = Chunk<T>::from(c + (g / (N / 4) * 256 + tid) * N, a.C) + g % (N / 4) * 4;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    if (w[j] >= reach) list[count + __builtin_amdgcn_mbcnt_hi((unsigned)(mask[j] >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)mask[j], 0))] =
+                        make_float2(w[j], __builtin_bit_cast(float, from + j));
+                    count += __popcll(mask[j]);
+                }
+            }
+            if (!full) break;
+            cut();
+        }
     }
-    Sums k{lanes_max<64>(best), 0.f, 0.f};
-    const float m = centre(k.m);
-#pragma unroll
-    for (int u = 0; u < U; ++u)
-#pragma unroll
-        for (int j = 0; j < N; ++j) add_score(k, v[u][j], m);
-    k.s = lanes_sum<64>(k.s);
-    k.u = lanes_sum<64>(k.u);
-    const float bound = a.top ? reached_by(best, a.top) : 0.f;
+    if (count > LISTS_JOINED / 4) cut();
+    Sums all{lanes_max<64>(k.m), 0.f, 0.f};
+    {
+        const float d = fmaxf((k.m - centre(all.m)) * LOG2E, MASKED), e = __builtin_amdgcn_exp2f(d);
+        all.s = lanes_sum<64>(k.s * e);
+        all.u = lanes_sum<64>((k.u + k.s * d) * e) * LN2;
+    }
     if (tid == 0) s_count = 0;
     if (lane == 0) {
-        s_sums[wave] = k;
+        s_sums[wave] = all;
         s_bound[wave] = bound;
     }
     __syncthreads();
@@ -222,87 +372,42 @@ __global__ __launch_bounds__(256) void logp_part_kernel(const T *__restrict__ x,
         else *(Sums *)((char *)p.sums + (row * p.parts + part) * SUMS_BYTES) = k;
     }
     if (a.top == 0) return;
-    const float least = fmaxf(fmaxf(s_bound[0], s_bound[1]), fmaxf(s_bound[2], s_bound[3]));
-#pragma unroll
-    for (int u = 0; u < U; ++u)
-        if (__any(most[u] >= least && most[u] > -INFINITY)) {
-#pragma unroll
-            for (int j = 0; j < N; ++j)
-                if (v[u][j] >= least && v[u][j] > -INFINITY) {
-                    const int i = atomicAdd(&s_count, 1);
-                    if (i < PART_LIST) {
-                        s_value[i] = v[u][j];
-                        s_from[i] = c0 + u * 256 * N + j;
-                    }
-                }
-        }
+    bound = fmaxf(fmaxf(s_bound[0], s_bound[1]), fmaxf(s_bound[2], s_bound[3]));
+    for (int i = lane; i < count; i += 64) {
+        const float2 e = list[i];
+        if (e.x >= bound) s_joined[atomicAdd(&s_count, 1)] = e;
+    }
     __syncthreads();
     const int found = s_count;
     auto put = [&](int i, float value, int c) {
         if (p.parts == 1) store_top(a, row * a.top + i, value, c, k, log_s);
         else p.best[(row * p.parts + part) * a.top + i] = make_float2(value, __builtin_bit_cast(float, c));
     };
-    if (found <= PART_LIST) {
-        for (int i = tid; i < found; i += 256) {
-            const float value = s_value[i];
-            const int c = s_from[i];
-            int rank = 0;
-            for (int o = 0; o < found; ++o) rank += s_value[o] > value || (s_value[o] == value && s_from[o] < c);
-            if (rank < a.top) put(rank, value, c);
-        }
-        for (int i = found + tid; i < a.top; i += 256) put(i, -INFINITY, NO_CLASS);
-        return;
-    }
-    for (int i = 0; i < a.top; ++i) {
-        best = -INFINITY;
-        int c = NO_CLASS;
-#pragma unroll
-        for (int u = 0; u < U; ++u)
-#pragma unroll
-            for (int j = 0; j < N; ++j) best = fmaxf(best, v[u][j]);
-        best = lanes_max<64>(best);
-#pragma unroll
-        for (int u = U - 1; u >= 0; --u)
-#pragma unroll
-            for (int j = N - 1; j >= 0; --j)
-                if (v[u][j] == best) c = c0 + u * 256 * N + j;
-        c = lanes_min<64>(c);
-        if (lane == 0) {
-            s_best[wave] = best;
-            s_class[wave] = c;
-        }
-        __syncthreads();
-        best = s_best[0];
-        c = s_class[0];
-        for (int w = 1; w < 4; ++w)
-            if (s_best[w] > best || (s_best[w] == best && s_class[w] < c)) {
-                best = s_best[w];
-                c = s_class[w];
-            }
-        __syncthreads();
-        if (tid == 0) put(i, best, c);
-#pragma unroll
-        for (int u = 0; u < U; ++u)
-#pragma unroll
-            for (int j = 0; j < N; ++j)
-                if (c0 + u * 256 * N + j == c) v[u][j] = -INFINITY;
-    }
+    each_ranked(s_joined, found, tid, 256, [&](int rank, float value, int c) {
+        if (rank < a.top) put(rank, value, c);
+    });
+    for (int i = found + tid; i < a.top; i += 256) put(i, -INFINITY, NO_CLASS);
 }
 
-// The parts of a row, one to a lane of the row's wave: sums joined, lists (each in order) merged by their heads.
+// The parts of a row, one to a lane of the row's wave: sums joined, and the alternatives as in a part: the lanes look at the first 64 of
+// the parts' best, second best and so on, the `top`-th largest of those is reached by at least as many, and what reaches it
+// goes to a list.
 constexpr int PARTS_MAX = 64;
 template <class T>
 __global__ __launch_bounds__(64) void logp_join_kernel(const T *__restrict__ x, LogpArgs a, LogpParts p)
 {
-    extern __shared__ float2 s_lists[];          // [parts][top]
+    __shared__ float2 s_list[PARTS_MAX * FLEX_LOGP_MAX_TOP + 8];
+    __shared__ int s_count;
     const int lane = threadIdx.x;
     const int64_t row = blockIdx.x;
     const int t = a.target ? a.target[row] : 0;
     if (ignored(a, t)) return;
-    const float target_score = lane == 0 && a.target ? to_f32(x[row / a.N * a.bs + row % a.N * a.ps + t]) : 0.f;
+    const float target_score = lane == 0 && a.target ? to_f32(x[row * a.stride + t]) : 0.f;
     Sums k = lane < p.parts ? *(const Sums *)((const char *)p.sums + (row * p.parts + lane) * SUMS_BYTES) : Sums{-INFINITY, 0.f, 0.f};
     const float2 *lists = p.best + row * p.parts * a.top;
-    for (int i = lane; i < p.parts * a.top; i += 64) s_lists[i] = lists[i];
+    const int entries = p.parts * a.top, depth = 64 / p.parts;
+    const float seen = a.top && lane < depth * p.parts && lane / p.parts < a.top ? lists[lane % p.parts * a.top + lane / p.parts].x : -INFINITY;
+    if (lane == 0) s_count = 0;
     const Sums all{lanes_max<64>(k.m), 0.f, 0.f};
     k = joined(k, all);
     k.s = lanes_sum<64>(k.s);
@@ -311,19 +416,18 @@ __global__ __launch_bounds__(64) void logp_join_kernel(const T *__restrict__ x, 
     const float log_s = logf(k.s);
     if (lane == 0) store_sums(a, row, target_score, k, log_s);
     if (a.top == 0) return;
+    const float least = reached_by(seen, a.top);
     __syncthreads();
-    int at = lane * a.top, end = lane < p.parts ? at + a.top : at;
-    float2 head = at < end ? s_lists[at] : make_float2(-INFINITY, __builtin_bit_cast(float, NO_CLASS));
-    for (int i = 0; i < a.top; ++i) {
-        const float best = lanes_max<64>(head.x);
-        const int own = __builtin_bit_cast(int, head.y);
-        const int c = lanes_min<64>(head.x == best ? own : NO_CLASS);
-        if (lane == 0) store_top(a, row * a.top + i, best, c, k, log_s);
-        if (own == c && head.x == best) {
-            ++at;
-            head = at < end ? s_lists[at] : make_float2(-INFINITY, __builtin_bit_cast(float, NO_CLASS));
-        }
+    for (int i = lane; i < entries; i += 64) {
+        const float2 e = lists[i];
+        if (e.x >= least && e.x > -INFINITY) s_list[atomicAdd(&s_count, 1)] = e;
     }
+    __syncthreads();
+    const int found = s_count;
+    each_ranked(s_list, found, lane, 64, [&](int rank, float value, int c) {
+        if (rank < a.top) store_top(a, row * a.top + rank, value, c, k, log_s);
+    });
+    for (int i = found + lane; i < a.top; i += 64) store_top(a, row * a.top + i, -INFINITY, NO_CLASS, k, log_s);
 }
 
 // ---- channel-major --------------------------------------------------------------------------------------------------------
@@ -336,20 +440,21 @@ __global__ __launch_bounds__(64 * W) void logp_cols_kernel(const T *__restrict__
     __shared__ float s_best[W][64];
     __shared__ int s_class[W][64];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t tiles = (a.N + 63) / 64, b = blockIdx.x / tiles;
+    const unsigned tiles = (unsigned)(a.N + 63) / 64;
+    const int64_t b = blockIdx.x / tiles;
     const int n = (int)(blockIdx.x % tiles) * 64 + lane;
     const bool mine = n < a.N;
     const int64_t row = b * a.N + n;
     const int t = mine && a.target ? a.target[row] : 0;
     const bool skip = !mine || ignored(a, t);
-    const T *at = x + b * a.bs + n;
+    const T *at = x + b * a.C * a.stride + n;
     const int per = R ? R : (a.C + W - 1) / W, first = wave * per, last = min(first + per, a.C);
     float v[R ? R : 1];
     Sums k{-INFINITY, 0.f, 0.f};
     float best = -INFINITY;
     if (R) {
 #pragma unroll
-        for (int i = 0; i < R; ++i) v[i] = !skip && first + i < last ? to_f32(at[(first + i) * a.cs]) : -INFINITY;
+        for (int i = 0; i < R; ++i) v[i] = !skip && first + i < last ? to_f32(at[(first + i) * a.stride]) : -INFINITY;
 #pragma unroll
         for (int i = 0; i < R; ++i) best = fmaxf(best, v[i]);
         k.m = best;
@@ -357,10 +462,10 @@ __global__ __launch_bounds__(64 * W) void logp_cols_kernel(const T *__restrict__
 #pragma unroll
         for (int i = 0; i < R; ++i) add_score(k, v[i], m);
     } else if (!skip) {
-        for (int c = first; c < last; ++c) best = fmaxf(best, to_f32(at[c * a.cs]));
+        for (int c = first; c < last; ++c) best = fmaxf(best, to_f32(at[c * a.stride]));
         k.m = best;
         const float m = centre(best);
-        for (int c = first; c < last; ++c) add_score(k, to_f32(at[c * a.cs]), m);
+        for (int c = first; c < last; ++c) add_score(k, to_f32(at[c * a.stride]), m);
     }
     if (W > 1) {
         s_sums[wave][lane] = k;
@@ -373,7 +478,7 @@ __global__ __launch_bounds__(64 * W) void logp_cols_kernel(const T *__restrict__
     const float log_s = logf(k.s);
     if (wave == 0 && mine) {
         if (skip) a.logp[row] = a.entropy[row] = a.lse[row] = 0.f;
-        else store_sums(a, row, a.target ? to_f32(at[t * a.cs]) : 0.f, k, log_s);
+        else store_sums(a, row, a.target ? to_f32(at[t * a.stride]) : 0.f, k, log_s);
     }
     float last_best = INFINITY;
     int last_class = -1;
@@ -386,7 +491,7 @@ __global__ __launch_bounds__(64 * W) void logp_cols_kernel(const T *__restrict__
                 if (v[r] > best) { best = v[r]; c = first + r; }
         } else if (!skip) {
             for (int r = first; r < last; ++r) {
-                const float y = to_f32(at[r * a.cs]);
+                const float y = to_f32(at[r * a.stride]);
                 if (y > best && (y < last_best || (y == last_best && r > last_class))) { best = y; c = r; }
             }
         }
@@ -416,7 +521,7 @@ __global__ __launch_bounds__(64 * W) void logp_cols_kernel(const T *__restrict__
 struct LogpBwdArgs {
     const int32_t *target;
     const float *lse, *entropy, *grad_logp, *grad_entropy;
-    int64_t rows, bs, ps, cs, gbs, gps, gcs;     // strides of the scores and of their gradient
+    int64_t rows, stride, grad_stride;           // positions; elements from row to row of the scores and of their gradient
     int N, C;
 };
 struct LogpBwdRow {
@@ -447,49 +552,50 @@ __global__ __launch_bounds__(256) void logp_bwd_rows_kernel(const T *x, T *gx, L
     constexpr int N = LANE_ELEMENTS<T>;
     const int64_t row = L == 256 ? blockIdx.x / chunks : (int64_t)blockIdx.x * (256 / L) + threadIdx.x / L;
     if (row >= a.rows) return;
-    const int64_t b = row / a.N, n = row % a.N;
-    const T *at = x + b * a.bs + n * a.ps;
-    T *to = gx + b * a.gbs + n * a.gps;
+    const T *at = x + row * a.stride;
+    T *to = gx + row * a.grad_stride;
     const int c0 = ((L == 256 ? (int)(blockIdx.x % chunks) * U * L : 0) + (int)(threadIdx.x % L)) * N;
     const LogpBwdRow f(a, row);
     float v[U][N];
+    // (in place no lane may read what another one writes: the row's end is read element by element, after all else has been asked for)
+    typename Chunk<T>::V raw[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+        if (!f.zero && c0 + u * L * N + N <= a.C) raw[u] = *(const typename Chunk<T>::V *)(at + c0 + u * L * N);
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-        if (f.zero) {
+        const int c = c0 + u * L * N;
+        if (!f.zero && c < a.C && c + N > a.C)
 #pragma unroll
-            for (int j = 0; j < N; ++j) v[u][j] = 0.f;
-        } else
-            Chunk<T>::load_row(at, c0 + u * L * N, a.C, v[u], 0.f);
-    }
+            for (int j = 0; j < N; ++j)
+                if (c + j < a.C) raw[u][j] = at[c + j];
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-        if (!f.zero)
-#pragma unroll
-            for (int j = 0; j < N; ++j) v[u][j] = f(v[u][j], c0 + u * L * N + j);
-        Chunk<T>::store_row(to, c0 + u * L * N, a.C, v[u]);
+        for (int j = 0; j < N; ++j) v[u][j] = f.zero ? 0.f : f(to_f32(raw[u][j]), c + j);
+        Chunk<T>::store_row(to, c, a.C, v[u]);
     }
 }
 
 // Channel-major: a lane to a position, a workgroup to 256 of them and 16 classes.
 constexpr int BWD_CLASSES = 16;
 template <class T>
-__global__ __launch_bounds__(256) void logp_bwd_cols_kernel(const T *x, T *gx, LogpBwdArgs a, int tiles, int parts)
+__global__ __launch_bounds__(256) void logp_bwd_cols_kernel(const T *x, T *gx, LogpBwdArgs a, unsigned tiles, unsigned parts)
 {
-    const int part = blockIdx.x % parts, tile = blockIdx.x / parts % tiles;
+    const unsigned part = blockIdx.x % parts, tile = blockIdx.x / parts % tiles;
     const int64_t b = blockIdx.x / parts / tiles;
     const int n = tile * 256 + threadIdx.x;
     if (n >= a.N) return;
     const int first = part * BWD_CLASSES, many = min(BWD_CLASSES, a.C - first);
-    const T *at = x + b * a.bs + first * a.cs + n;
-    T *to = gx + b * a.gbs + first * a.gcs + n;
+    const T *at = x + (b * a.C + first) * a.stride + n;
+    T *to = gx + (b * a.C + first) * a.grad_stride + n;
+    // (an ignored position's scores share their lines with its neighbours': nothing is saved by not reading them)
+    T v[BWD_CLASSES];
+#pragma unroll
+    for (int i = 0; i < BWD_CLASSES; ++i)
+        if (i < many) v[i] = at[i * a.stride];
     const LogpBwdRow f(a, b * a.N + n);
-    float v[BWD_CLASSES];
 #pragma unroll
     for (int i = 0; i < BWD_CLASSES; ++i)
-        if (i < many && !f.zero) v[i] = to_f32(at[i * a.cs]);
-#pragma unroll
-    for (int i = 0; i < BWD_CLASSES; ++i)
-        if (i < many) to[i * a.gcs] = (T)(f.zero ? 0.f : f(v[i], first + i));
+        if (i < many) to[i * a.grad_stride] = (T)(f.zero ? 0.f : f(to_f32(v[i]), first + i));
 }
 
 // ---- launches -------------------------------------------------------------------------------------------------------------
@@ -508,24 +614,17 @@ static hipError_t with_row_lanes(int C, F f)
 }
 static int row_columns_max(int dtype) { return 2048 / (int)dtype_bytes(dtype); }      // 64 lanes x 2 x 16 bytes
 
-// How a long row is cut: 16-byte pieces a thread takes (2, 4 or 8, fp32 16), the longest with which there are two workgroups to a
-// compute unit, and enough that a row has at most PARTS_MAX parts.
+// How a long row is cut: into parts of whole spans, so many that there are eight workgroups to a compute unit, or that a part is one
+// span, at most PARTS_MAX.
 struct PartPlan {
-    int U, parts;
+    int parts, spans;
 };
 static PartPlan plan_parts(int64_t rows, int C, int dtype)
 {
-    const int lane = 16 / (int)dtype_bytes(dtype);
-    PartPlan p{};
-    for (p.U = 16; ; p.U /= 2) {
-        p.parts = (int)cdiv64(C, 256 * lane * p.U);
-        if (p.U == 2 || (rows * p.parts >= 2 * device_cu_count() && (dtype == FLEX_F32 || p.U < 16))) break;
-    }
-    while (p.parts > PARTS_MAX) {
-        p.U *= 2;
-        p.parts = (int)cdiv64(C, 256 * lane * p.U);
-    }
-    return p;
+    const int span = 256 * SPAN_LOADS * (16 / (int)dtype_bytes(dtype)), all = (int)cdiv64(C, span);
+    const int wanted = (int)std::min<int64_t>(std::min(all, PARTS_MAX), std::max<int64_t>(1, 8 * device_cu_count() / rows));
+    const int spans = (int)cdiv64(all, wanted);
+    return PartPlan{(int)cdiv64(all, spans), spans};
 }
 static size_t parts_sums_bytes(int64_t rows, int parts) { return align256((size_t)rows * parts * SUMS_BYTES); }
 
@@ -535,18 +634,20 @@ static hipError_t launch_logp_rows(const T *x, const LogpArgs &a, int dtype, voi
     if (a.C <= row_columns_max(dtype))
         return with_row_lanes<T>(a.C, [&](auto l, auto u) {
             constexpr int L = decltype(l)::value, U = decltype(u)::value;
-            hipLaunchKernelGGL((logp_rows_kernel<T, L, U>), dim3((unsigned)cdiv64(a.rows, 256 / L)), dim3(256), 0, s, x, a);
+            const dim3 grid((unsigned)cdiv64(a.rows, 256 / L));
+            if constexpr (L == 4)
+                if (a.C < LANE_ELEMENTS<T>) {
+                    hipLaunchKernelGGL((logp_rows_kernel<T, L, U, true>), grid, dim3(256), 0, s, x, a);
+                    return hipGetLastError();
+                }
+            hipLaunchKernelGGL((logp_rows_kernel<T, L, U, false>), grid, dim3(256), 0, s, x, a);
             return hipGetLastError();
         });
     const PartPlan q = plan_parts(a.rows, a.C, dtype);
-    const LogpParts p{(Sums *)ws, (float2 *)((char *)ws + parts_sums_bytes(a.rows, q.parts)), q.parts};
-    const dim3 grid((unsigned)(a.rows * q.parts)), wg(256);
-    if (q.U == 2) hipLaunchKernelGGL((logp_part_kernel<T, 2>), grid, wg, 0, s, x, a, p);
-    else if (q.U == 4) hipLaunchKernelGGL((logp_part_kernel<T, 4>), grid, wg, 0, s, x, a, p);
-    else if (q.U == 8) hipLaunchKernelGGL((logp_part_kernel<T, 8>), grid, wg, 0, s, x, a, p);
-    else if constexpr (sizeof(T) == 4) hipLaunchKernelGGL((logp_part_kernel<T, 16>), grid, wg, 0, s, x, a, p);
+    const LogpParts p{(Sums *)ws, (float2 *)((char *)ws + parts_sums_bytes(a.rows, q.parts)), q.parts, q.spans};
+    hipLaunchKernelGGL(logp_part_kernel<T>, dim3((unsigned)(a.rows * q.parts)), dim3(256), 0, s, x, a, p);
     if (q.parts > 1)
-        hipLaunchKernelGGL(logp_join_kernel<T>, dim3((unsigned)a.rows), dim3(64), sizeof(float2) * q.parts * a.top, s, x, a, p);
+        hipLaunchKernelGGL(logp_join_kernel<T>, dim3((unsigned)a.rows), dim3(64), 0, s, x, a, p);
     return hipGetLastError();
 }
 
@@ -566,9 +667,8 @@ template <class T>
 static hipError_t launch_logp_bwd(const T *x, T *gx, const LogpBwdArgs &a, int B, bool bcn, int dtype, hipStream_t s)
 {
     if (bcn) {
-        const int tiles = (a.N + 255) / 256, parts = (a.C + BWD_CLASSES - 1) / BWD_CLASSES;
+        const unsigned tiles = (unsigned)(a.N + 255) / 256, parts = (unsigned)(a.C + BWD_CLASSES - 1) / BWD_CLASSES;
         const int64_t grid = (int64_t)B * tiles * parts;
-        if (grid >= ((int64_t)1 << 31)) return hipErrorInvalidValue;
         hipLaunchKernelGGL(logp_bwd_cols_kernel<T>, dim3((unsigned)grid), dim3(256), 0, s, x, gx, a, tiles, parts);
         return hipGetLastError();
     }
@@ -618,8 +718,7 @@ int flexlogp_fwd(const void *logits, const int32_t *target, float *logp, float *
     if (!workspace || ((uintptr_t)workspace & 255) || workspace_bytes < flexlogp_fwd_workspace_bytes(B, N, C, top, dtype, layout))
         return FLEX_ERR_WORKSPACE;
     const bool bcn = layout == FLEX_LAYOUT_BCN;
-    const LogpArgs a{target, logp, entropy, lse, top_logp, top_class, (int64_t)B * N, (bcn ? C : N) * row_stride,
-                     bcn ? 1 : row_stride, bcn ? row_stride : 1, N, C, top};
+    const LogpArgs a{target, logp, entropy, lse, top_logp, top_class, (int64_t)B * N, row_stride, N, C, top};
     const hipError_t e = with_dtype(dtype, [&](auto t) {
         typedef decltype(t) T;
         return bcn ? launch_logp_cols<T>((const T *)logits, a, B, (hipStream_t)stream)
@@ -637,9 +736,7 @@ int flexlogp_bwd(const void *logits, const int32_t *target, const float *lse, co
     if (!logp_sizes_ok(B, N, C, row_stride, dtype, layout) || !logp_sizes_ok(B, N, C, grad_row_stride, dtype, layout)) return FLEX_ERR_SHAPE;
     if (logits == grad_logits && row_stride != grad_row_stride) return FLEX_ERR_SHAPE;
     const bool bcn = layout == FLEX_LAYOUT_BCN;
-    const LogpBwdArgs a{target, lse, entropy, grad_logp, grad_entropy, (int64_t)B * N,
-                        (bcn ? C : N) * row_stride, bcn ? 1 : row_stride, bcn ? row_stride : 1,
-                        (bcn ? C : N) * grad_row_stride, bcn ? 1 : grad_row_stride, bcn ? grad_row_stride : 1, N, C};
+    const LogpBwdArgs a{target, lse, entropy, grad_logp, grad_entropy, (int64_t)B * N, row_stride, grad_row_stride, N, C};
     const hipError_t e = with_dtype(dtype, [&](auto t) {
         typedef decltype(t) T;
         return launch_logp_bwd<T>((const T *)logits, (T *)grad_logits, a, B, bcn, dtype, (hipStream_t)stream);
