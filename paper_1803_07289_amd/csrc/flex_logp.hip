@@ -27,14 +27,24 @@ struct LogpArgs {
 struct Sums {
     float m, s, u;
 };
-// sums about a.m and b.m as one
-__device__ __forceinline__ Sums joined(const Sums &a, const Sums &b)
+// m as the sums are taken about it: an empty position's is no number to subtract
+__device__ __forceinline__ float centre(float m) { return m == -INFINITY ? 0.f : m; }
+
+// The sums of n, each about its own m, as one about the largest.
+template <int n>
+__device__ __forceinline__ Sums joined(const Sums (&k)[n])
 {
-    const float m = fmaxf(a.m, b.m);
-    if (m == -INFINITY) return Sums{m, a.s + b.s, 0.f};
-    const float da = fmaxf(a.m - m, MASKED), db = fmaxf(b.m - m, MASKED);
-    const float ea = __builtin_amdgcn_exp2f(da * LOG2E), eb = __builtin_amdgcn_exp2f(db * LOG2E);
-    return Sums{m, a.s * ea + b.s * eb, (a.u + a.s * da) * ea + (b.u + b.s * db) * eb};
+    Sums all{k[0].m, 0.f, 0.f};
+#pragma unroll
+    for (int i = 1; i < n; ++i) all.m = fmaxf(all.m, k[i].m);
+    const float m = centre(all.m);
+#pragma unroll
+    for (int i = 0; i < n; ++i) {
+        const float d = fmaxf(k[i].m - m, MASKED), e = __builtin_amdgcn_exp2f(d * LOG2E);
+        all.s += k[i].s * e;
+        all.u += (k[i].u + k[i].s * d) * e;
+    }
+    return all;
 }
 __device__ __forceinline__ void add_score(Sums &a, float x, float m)
 {
@@ -42,9 +52,6 @@ __device__ __forceinline__ void add_score(Sums &a, float x, float m)
     a.s += e;
     a.u += e * fmaxf(z, MASKED);
 }
-// m as the sums are taken about it: an empty position's is no number to subtract
-__device__ __forceinline__ float centre(float m) { return m == -INFINITY ? 0.f : m; }
-
 __device__ __forceinline__ void store_sums(const LogpArgs &a, int64_t row, float target_score, const Sums &k, float log_s)
 {
     if (a.target) a.logp[row] = k.s == 0.f ? -INFINITY : target_score - k.m - log_s;
@@ -141,57 +148,65 @@ __global__ __launch_bounds__(256) void logp_rows_kernel(const T *__restrict__ x,
 // step.
 // Alternatives: the `top`-th largest of a wave's 64 lane maxima so far is reached by `top` of its scores, so only what reaches it
 // can be among the best; that goes to the wave's list in LDS, some two `top`s in most rows.  A list that fills up (rows of equal
-// scores, ascending rows) is cut to the best `top`, after which, since a wave meets its classes in ascending order (but for the two
-// halves of 16-bit pieces), later scores have to exceed the last of them.  The lists meet in one, cut by the largest bound of the four waves, and are ranked there.  Parts
-// of one row meet in logp_join_kernel.
+// scores, ascending rows) is cut to the best `top`; scores of later spans then have to exceed the last of them.  The lists meet in
+// one, cut by the largest bound of the four waves, and are ranked there.  Parts of one row meet in logp_join_kernel.
+// The path of the candidates is loops over few instructions, which read the scores again, from the cache: unrolled over the registers
+// it was 5 KB of code that a call for one token waits for line by line (one row of 131072, top 20: 15 us, without alternatives 3.7).
 
-// the bits of a float, ordered like the floats
+// the bits of a float, ordered like the floats (of the two zeros the positive one: they are equal)
 __device__ __forceinline__ uint32_t order_key(float v)
 {
-    const uint32_t b = __builtin_bit_cast(uint32_t, v);
+    const uint32_t b = __builtin_bit_cast(uint32_t, v + 0.f);
     return b ^ ((uint32_t)((int32_t)b >> 31) | 0x80000000u);
 }
 __device__ __forceinline__ float from_order_key(uint32_t k)
 {
     return __builtin_bit_cast(float, k ^ (k >> 31 ? 0x80000000u : 0xFFFFFFFFu));
 }
+// A candidate as one number, the better ones the larger: the score, then the class, lower ones first.
+typedef unsigned long long Candidate;
+__device__ __forceinline__ Candidate candidate(float v, int c) { return (Candidate)order_key(v) << 32 | (uint32_t)~c; }
+__device__ __forceinline__ float score_of(Candidate e) { return from_order_key((uint32_t)(e >> 32)); }
+__device__ __forceinline__ int class_of(Candidate e) { return (int)~(uint32_t)e; }
 
-// A value that at least n of the wave's 64 lanes reach, the largest such one to within the last 12 bits; -inf if fewer are above -inf.
+// A value that at least n of the wave's 64 lanes reach, the largest such one to within the last 12 bits; -inf if fewer are above
+// -inf.  Two bits a step: three counts that do not wait for each other.
 __device__ __forceinline__ float reached_by(float v, int n)
 {
     const uint32_t key = order_key(v);
     uint32_t found = 0;
-#pragma unroll
-    for (int b = 31; b >= 12; --b) {
-        const uint32_t next = found | 1u << b;
-        if (__popcll(__ballot(key >= next)) >= n) found = next;
+#pragma unroll 1
+    for (int b = 30; b >= 12; b -= 2) {
+        const int one = __popcll(__ballot(key >= (found | 1u << b))), two = __popcll(__ballot(key >= (found | 2u << b))),
+                  three = __popcll(__ballot(key >= (found | 3u << b)));
+        found |= (three >= n ? 3u : two >= n ? 2u : one >= n ? 1u : 0u) << b;
     }
     return found <= order_key(-INFINITY) ? -INFINITY : from_order_key(found);
 }
 
-// Candidates for the alternatives in LDS, score and class (as bits).  f(place, score, class) for each of them, its place the number of
-// those before it, by `threads` threads; seven entries behind the list are read, and have to be there.
+// f(place, candidate) for each of a list in LDS, its place the number of those before it, by `threads` threads, four to a candidate.
+// The list's memory ends on a multiple of eight.
 template <class F>
-__device__ __forceinline__ void each_ranked(const float2 *list, int found, int tid, int threads, F f)
+__device__ __forceinline__ void each_ranked(const Candidate *list, int found, int tid, int threads, F f)
 {
-    for (int i = tid; i < found; i += threads) {
-        const float value = list[i].x;
-        const int c = __builtin_bit_cast(int, list[i].y);
+    for (int i = tid >> 2; i < ((found + 15) & ~15); i += threads >> 2) {      // (whole quads, and all lanes of a wave's quads)
+        const Candidate own = list[min(i, found - 1)];
         int rank = 0;
-        for (int o = 0; o < found; o += 8)
-#pragma unroll
-            for (int k = 0; k < 8; ++k) {
-                const float2 e = list[o + k];
-                rank += o + k < found && (e.x > value || (e.x == value && __builtin_bit_cast(int, e.y) < c));
-            }
-        f(rank, value, c);
+#pragma unroll 4
+        for (int o = 2 * (tid & 3); o < found; o += 8) {
+            const Candidate x = list[o], y = list[o + 1];
+            rank += (int)(x > own) + (int)((y > own) & (o + 1 < found));
+        }
+        rank += __builtin_amdgcn_update_dpp(0, rank, DPP_XOR1, 0xF, 0xF, true);
+        rank += __builtin_amdgcn_update_dpp(0, rank, DPP_XOR2, 0xF, 0xF, true);
+        if (i < found && (tid & 3) == 0) f(rank, own);
     }
 }
 
 // What a part leaves of itself: its sums and its best scores with their classes.
 struct LogpParts {
     Sums *sums;                       // [rows][parts], 16 bytes apart
-    float2 *best;                     // [rows][parts][top]: score, class (as bits)
+    Candidate *best;                  // [rows][parts][top], in order; 0: none
     int parts, spans;                 // parts of a row, spans of a part
 };
 constexpr int SUMS_BYTES = 16, SPAN_LOADS = 4;
@@ -235,8 +250,8 @@ __global__ __launch_bounds__(256) void logp_part_kernel(const T *__restrict__ x,
     __shared__ Sums s_sums[4];
     __shared__ float s_bound[4];
     __shared__ int s_count;
-    __shared__ float2 s_list[4][WAVE_LIST + 8], s_cut[4][FLEX_LOGP_MAX_TOP], s_joined[LISTS_JOINED + 8];
-    float2 *const list = s_list[wave];
+    __shared__ Candidate s_list[4][WAVE_LIST], s_cut[4][FLEX_LOGP_MAX_TOP], s_joined[LISTS_JOINED];
+    Candidate *const list = s_list[wave];
     const T *at = x + row * a.stride;
     const int begin = (int)part * p.spans * SPAN<T>, end = min(a.C, begin + p.spans * SPAN<T>);
     V next[U];
@@ -248,23 +263,21 @@ __global__ __launch_bounds__(256) void logp_part_kernel(const T *__restrict__ x,
     const float target_score = tid == 0 && a.target && p.parts == 1 ? to_f32(at[t]) : 0.f;
     Sums k{-INFINITY, 0.f, 0.f};       // of the lane; u in units of ln 2
     float least = LOWEST, bound = LOWEST;       // what a candidate reaches; what `top` scores of the wave are known to reach
-    float same = LOWEST;               // the last of a list that was cut, which a score of the piece at hand may equal
     int count = 0;                     // the wave's list
 
     // the list's best `top`, in order
     auto cut = [&]() {
         lds_in_order();
-        each_ranked(list, count, lane, 64, [&](int rank, float value, int c) {
-            if (rank < a.top) s_cut[wave][rank] = make_float2(value, __builtin_bit_cast(float, c));
+        each_ranked(list, count, lane, 64, [&](int rank, Candidate e) {
+            if (rank < a.top) s_cut[wave][rank] = e;
         });
         lds_in_order();
         if (count <= a.top) return;
         if (lane < a.top) list[lane] = s_cut[wave][lane];
         count = a.top;
-        const float last = s_cut[wave][a.top - 1].x;
+        const float last = score_of(s_cut[wave][a.top - 1]);
         bound = fmaxf(bound, last);
-        same = fmaxf(least, last);
-        least = fmaxf(least, from_order_key(order_key(last) + 1));
+        least = fmaxf(least, last);
         lds_in_order();
     };
 
@@ -320,36 +333,30 @@ __global__ __launch_bounds__(256) void logp_part_kernel(const T *__restrict__ x,
         if (a.top == 0 || !__any(span_most >= least)) continue;
         bound = fmaxf(bound, reached_by(k.m, a.top));
         least = fmaxf(least, bound);
-        for (int done = -1;;) {
-            bool full = false;
+        unsigned groups = 0;
 #pragma unroll
-            for (int g = 0; g < GROUPS; ++g) {
-                const float reach = g == done && g % (N / 4) ? same : least;
-                if (full || g < done || !__any(most[g] >= reach)) continue;
-                const float *w = &v[g / (N / 4)][g % (N / 4) * 4];
-                uint64_t mask[4];
-                int more = 0;
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    mask[j] = __ballot(w[j] >= reach);
-                    more += __popcll(mask[j]);
-                }
-                if (count + more > WAVE_LIST) {
-                    full = true;
-                    done = g;
-                    continue;
-                }
-                const int from = Chunk<T>::from(c + (g / (N / 4) * 256 + tid) * N, a.C) + g % (N / 4) * 4;
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    if (w[j] >= reach) list[count + __builtin_amdgcn_mbcnt_hi((unsigned)(mask[j] >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)mask[j], 0))] =
-                        make_float2(w[j], __builtin_bit_cast(float, from + j));
-                    count += __popcll(mask[j]);
-                }
+        for (int g = 0; g < GROUPS; ++g) groups |= most[g] >= least ? 1u << g : 0u;
+        bool was_cut = false;
+        while (const uint64_t lanes = __ballot(groups != 0)) {
+            if (count + 4 * __popcll(lanes) > WAVE_LIST) {
+                cut();
+                was_cut = true;
             }
-            if (!full) break;
-            cut();
+            const int g = groups ? __builtin_ctz(groups) : 0, own = c + (g / (N / 4) * 256 + tid) * N;
+            const int from = Chunk<T>::from(own, a.C) + g % (N / 4) * 4;
+            float w[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+            if (groups) Chunk<T, 4>::load(at + from, w);
+            groups &= groups - 1;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const bool take = w[j] >= least && from + j >= own;
+                const uint64_t mask = __ballot(take);
+                const int place = count + (int)__builtin_amdgcn_mbcnt_hi((unsigned)(mask >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)mask, 0));
+                if (take) list[place] = candidate(w[j], from + j);
+                count += __popcll(mask);
+            }
         }
+        if (was_cut) least = from_order_key(order_key(least) + 1);
     }
     if (count > LISTS_JOINED / 4) cut();
     Sums all{lanes_max<64>(k.m), 0.f, 0.f};
@@ -364,7 +371,7 @@ __global__ __launch_bounds__(256) void logp_part_kernel(const T *__restrict__ x,
         s_bound[wave] = bound;
     }
     __syncthreads();
-    k = joined(joined(s_sums[0], s_sums[1]), joined(s_sums[2], s_sums[3]));
+    k = joined(s_sums);
     k.m = p.parts == 1 ? centre(k.m) : k.m;
     const float log_s = logf(k.s);
     if (tid == 0) {
@@ -374,19 +381,19 @@ __global__ __launch_bounds__(256) void logp_part_kernel(const T *__restrict__ x,
     if (a.top == 0) return;
     bound = fmaxf(fmaxf(s_bound[0], s_bound[1]), fmaxf(s_bound[2], s_bound[3]));
     for (int i = lane; i < count; i += 64) {
-        const float2 e = list[i];
-        if (e.x >= bound) s_joined[atomicAdd(&s_count, 1)] = e;
+        const Candidate e = list[i];
+        if (score_of(e) >= bound) s_joined[atomicAdd(&s_count, 1)] = e;
     }
     __syncthreads();
     const int found = s_count;
-    auto put = [&](int i, float value, int c) {
-        if (p.parts == 1) store_top(a, row * a.top + i, value, c, k, log_s);
-        else p.best[(row * p.parts + part) * a.top + i] = make_float2(value, __builtin_bit_cast(float, c));
+    auto put = [&](int i, Candidate e) {
+        if (p.parts == 1) store_top(a, row * a.top + i, e ? score_of(e) : -INFINITY, class_of(e), k, log_s);
+        else p.best[(row * p.parts + part) * a.top + i] = e;
     };
-    each_ranked(s_joined, found, tid, 256, [&](int rank, float value, int c) {
-        if (rank < a.top) put(rank, value, c);
+    each_ranked(s_joined, found, tid, 256, [&](int rank, Candidate e) {
+        if (rank < a.top) put(rank, e);
     });
-    for (int i = found + tid; i < a.top; i += 256) put(i, -INFINITY, NO_CLASS);
+    for (int i = found + tid; i < a.top; i += 256) put(i, 0);
 }
 
 // The parts of a row, one to a lane of the row's wave: sums joined, and the alternatives as in a part: the lanes look at the first 64 of
@@ -396,7 +403,7 @@ constexpr int PARTS_MAX = 64;
 template <class T>
 __global__ __launch_bounds__(64) void logp_join_kernel(const T *__restrict__ x, LogpArgs a, LogpParts p)
 {
-    __shared__ float2 s_list[PARTS_MAX * FLEX_LOGP_MAX_TOP + 8];
+    __shared__ Candidate s_list[PARTS_MAX * FLEX_LOGP_MAX_TOP];
     __shared__ int s_count;
     const int lane = threadIdx.x;
     const int64_t row = blockIdx.x;
@@ -404,28 +411,26 @@ __global__ __launch_bounds__(64) void logp_join_kernel(const T *__restrict__ x, 
     if (ignored(a, t)) return;
     const float target_score = lane == 0 && a.target ? to_f32(x[row * a.stride + t]) : 0.f;
     Sums k = lane < p.parts ? *(const Sums *)((const char *)p.sums + (row * p.parts + lane) * SUMS_BYTES) : Sums{-INFINITY, 0.f, 0.f};
-    const float2 *lists = p.best + row * p.parts * a.top;
+    const Candidate *lists = p.best + row * p.parts * a.top;
     const int entries = p.parts * a.top, depth = 64 / p.parts;
-    const float seen = a.top && lane < depth * p.parts && lane / p.parts < a.top ? lists[lane % p.parts * a.top + lane / p.parts].x : -INFINITY;
+    const Candidate looked_at = lane < depth * p.parts && lane / p.parts < a.top ? lists[lane % p.parts * a.top + lane / p.parts] : 0;
     if (lane == 0) s_count = 0;
-    const Sums all{lanes_max<64>(k.m), 0.f, 0.f};
-    k = joined(k, all);
-    k.s = lanes_sum<64>(k.s);
-    k.u = lanes_sum<64>(k.u);
-    k.m = centre(k.m);
+    const float m = centre(lanes_max<64>(k.m));
+    const float d = fmaxf(k.m - m, MASKED), e = __builtin_amdgcn_exp2f(d * LOG2E);
+    k = Sums{m, lanes_sum<64>(k.s * e), lanes_sum<64>((k.u + k.s * d) * e)};
     const float log_s = logf(k.s);
     if (lane == 0) store_sums(a, row, target_score, k, log_s);
     if (a.top == 0) return;
-    const float least = reached_by(seen, a.top);
+    const float least = reached_by(looked_at ? score_of(looked_at) : -INFINITY, a.top);
     __syncthreads();
     for (int i = lane; i < entries; i += 64) {
-        const float2 e = lists[i];
-        if (e.x >= least && e.x > -INFINITY) s_list[atomicAdd(&s_count, 1)] = e;
+        const Candidate e = lists[i];
+        if (e && score_of(e) >= least) s_list[atomicAdd(&s_count, 1)] = e;
     }
     __syncthreads();
     const int found = s_count;
-    each_ranked(s_list, found, lane, 64, [&](int rank, float value, int c) {
-        if (rank < a.top) store_top(a, row * a.top + rank, value, c, k, log_s);
+    each_ranked(s_list, found, lane, 64, [&](int rank, Candidate e) {
+        if (rank < a.top) store_top(a, row * a.top + rank, score_of(e), class_of(e), k, log_s);
     });
     for (int i = found + lane; i < a.top; i += 64) store_top(a, row * a.top + i, -INFINITY, NO_CLASS, k, log_s);
 }
@@ -470,9 +475,10 @@ __global__ __launch_bounds__(64 * W) void logp_cols_kernel(const T *__restrict__
     if (W > 1) {
         s_sums[wave][lane] = k;
         __syncthreads();
-        k = s_sums[0][lane];
+        Sums all[W];
 #pragma unroll
-        for (int w = 1; w < W; ++w) k = joined(k, s_sums[w][lane]);
+        for (int w = 0; w < W; ++w) all[w] = s_sums[w][lane];
+        k = joined(all);
     }
     k.m = centre(k.m);
     const float log_s = logf(k.s);
@@ -644,7 +650,7 @@ static hipError_t launch_logp_rows(const T *x, const LogpArgs &a, int dtype, voi
             return hipGetLastError();
         });
     const PartPlan q = plan_parts(a.rows, a.C, dtype);
-    const LogpParts p{(Sums *)ws, (float2 *)((char *)ws + parts_sums_bytes(a.rows, q.parts)), q.parts, q.spans};
+    const LogpParts p{(Sums *)ws, (Candidate *)((char *)ws + parts_sums_bytes(a.rows, q.parts)), q.parts, q.spans};
     hipLaunchKernelGGL(logp_part_kernel<T>, dim3((unsigned)(a.rows * q.parts)), dim3(256), 0, s, x, a, p);
     if (q.parts > 1)
         hipLaunchKernelGGL(logp_join_kernel<T>, dim3((unsigned)a.rows), dim3(64), 0, s, x, a, p);
@@ -705,7 +711,7 @@ size_t flexlogp_fwd_workspace_bytes(int B, int N, int C, int top, int dtype, int
     if (layout == FLEX_LAYOUT_BCN || C <= row_columns_max(dtype)) return 256;
     const int64_t rows = (int64_t)B * N;
     const int parts = plan_parts(rows, C, dtype).parts;
-    return parts == 1 ? 256 : parts_sums_bytes(rows, parts) + align256((size_t)rows * parts * top * sizeof(float2));
+    return parts == 1 ? 256 : parts_sums_bytes(rows, parts) + align256((size_t)rows * parts * top * sizeof(Candidate));
 }
 
 int flexlogp_fwd(const void *logits, const int32_t *target, float *logp, float *entropy, float *lse, float *top_logp,
