@@ -146,12 +146,12 @@ __global__ __launch_bounds__(256) void logp_rows_kernel(const T *__restrict__ x,
 // maximum so far and meet at the end.  What an element costs decides beside the memory (bf16: 2 bytes in the time of some 11 vector
 // operations): exp counts four, the product and difference in front of it are one fused operation, the maximum takes two elements a
 // step.
-// Alternatives: the `top`-th largest of a wave's 64 lane maxima so far is reached by `top` of its scores, so only what reaches it
-// can be among the best; that goes to the wave's list in LDS, some two `top`s in most rows.  A list that fills up (rows of equal
-// scores, ascending rows) is cut to the best `top`; scores of later spans then have to exceed the last of them.  The lists meet in
-// one, cut by the largest bound of the four waves, and are ranked there.  Parts of one row meet in logp_join_kernel.
-// The path of the candidates is loops over few instructions, which read the scores again, from the cache: unrolled over the registers
-// it was 5 KB of code that a call for one token waits for line by line (one row of 131072, top 20: 15 us, without alternatives 3.7).
+// Alternatives: the `top`-th largest of the 64 maxima that four lanes each have met so far is reached by `top` scores of the part, so
+// only what reaches it can be among the best; that goes to the wave's list in LDS.  The bound is found after the first span and
+// renewed when as many again have passed, from whatever maxima the other waves have left by then: each is a score of the part,
+// and an older one is a lower bound too.  A list that fills up (rows of equal scores, ascending rows) is cut to the best `top`;
+// scores of later spans then have to exceed the last of them.  The lists meet in one, cut by the largest bound of the four waves,
+// and are ranked there.  Parts of one row meet in logp_join_kernel.
 
 // the bits of a float, ordered like the floats (of the two zeros the positive one: they are equal)
 __device__ __forceinline__ uint32_t order_key(float v)
@@ -249,6 +249,7 @@ __global__ __launch_bounds__(256) void logp_part_kernel(const T *__restrict__ x,
     }
     __shared__ Sums s_sums[4];
     __shared__ float s_bound[4];
+    __shared__ volatile float s_most[64];
     __shared__ int s_count;
     __shared__ Candidate s_list[4][WAVE_LIST], s_cut[4][FLEX_LOGP_MAX_TOP], s_joined[LISTS_JOINED];
     Candidate *const list = s_list[wave];
@@ -257,13 +258,13 @@ __global__ __launch_bounds__(256) void logp_part_kernel(const T *__restrict__ x,
     V next[U];
     auto request = [&](int c) {
 #pragma unroll
-        for (int u = 0; u < U; ++u) next[u] = *(const V *)(at + Chunk<T>::from(c + (u * 256 + tid) * N, a.C));
+        for (int u = 0; u < U; ++u) next[u] = __builtin_nontemporal_load((const V *)(at + Chunk<T>::from(c + (u * 256 + tid) * N, a.C)));
     };
     request(begin);
     const float target_score = tid == 0 && a.target && p.parts == 1 ? to_f32(at[t]) : 0.f;
     Sums k{-INFINITY, 0.f, 0.f};       // of the lane; u in units of ln 2
     float least = LOWEST, bound = LOWEST;       // what a candidate reaches; what `top` scores of the wave are known to reach
-    int count = 0;                     // the wave's list
+    int count = 0, renew = begin;      // the wave's list; where its bound is due
 
     // the list's best `top`, in order
     auto cut = [&]() {
@@ -330,9 +331,15 @@ __global__ __launch_bounds__(256) void logp_part_kernel(const T *__restrict__ x,
         }
         k.s += s[0] + s[1];
         k.u += q[0] + q[1];
-        if (a.top == 0 || !__any(span_most >= least)) continue;
-        bound = fmaxf(bound, reached_by(k.m, a.top));
-        least = fmaxf(least, bound);
+        if (a.top == 0 || !(c == begin || __any(span_most >= least))) continue;
+        if (c >= renew) {
+            const float four = lanes_max<4>(k.m);
+            if ((lane & 3) == 0) s_most[tid >> 2] = four;
+            if (c == begin) __syncthreads();
+            bound = fmaxf(bound, reached_by(s_most[lane], a.top));
+            least = fmaxf(least, bound);
+            renew = c + (c - begin) + SPAN<T>;
+        }
         unsigned groups = 0;
 #pragma unroll
         for (int g = 0; g < GROUPS; ++g) groups |= most[g] >= least ? 1u << g : 0u;
