@@ -448,9 +448,11 @@ int flexnorm_bwd(const void *x, const void *weight, const void *grad_out, const 
  * lse are NaN, NaN is never an alternative.
  * row_stride (elements): point-major from one position's scores to the next one's, at least C (rows of a padded vocabulary);
  * channel-major from one class's scores to the next one's, at least N.  C <= FLEX_LOGP_MAX_CLASSES.
+ * Long rows that are few are cut in parts, which meet in the workspace; FLEX_LOGP_NO_WORKSPACE bytes: not so, workspace may be NULL.
  */
 #define FLEX_LOGP_MAX_CLASSES (1 << 20)
 #define FLEX_LOGP_MAX_TOP 32
+#define FLEX_LOGP_NO_WORKSPACE 256
 size_t flexlogp_fwd_workspace_bytes(int B, int N, int C, int top, int dtype, int layout);
 int flexlogp_fwd(const void *logits, const int32_t *target, float *logp, float *entropy, float *lse,
                  float *top_logp, int32_t *top_class, int B, int N, int C, int top, int64_t row_stride, int dtype,

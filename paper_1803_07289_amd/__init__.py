@@ -16,7 +16,7 @@ import torch
 
 # element types of the operators around the layers (flexnorm_*, flexlogp_*, flexadamw_*)
 _DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
-LOGP_MAX_TOP = 32
+LOGP_MAX_TOP, _LOGP_NO_WORKSPACE = 32, 256
 BCN = 0   # [B,C,N]  channel-major, the paper's form
 BNC = 1   # [B,N,C]  point-major, the library's native form
 OP_CONV_FWD, OP_CONV_BWD, OP_CONV_BWD_BUILD, OP_INEDGES, OP_UPSAMPLE = 0, 1, 2, 3, 4
@@ -655,14 +655,22 @@ def flex_validate_neighbors(nbr):
 
 # ---- the operators around the layers: layer norm, log probabilities, optimizer step -------------------------------------
 
-def _any(t, name, dtypes=_DTYPES):
-    """_dev for a tensor of one of the types `dtypes`, on the current device."""
+_current = torch._C._cuda_getDevice if hasattr(torch._C, "_cuda_getDevice") else torch.cuda.current_device
+
+
+def _here(t, name):
+    """Raises unless t is a tensor on the current device."""
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise TypeError(f"{name} must be a CUDA tensor")
+    if t.get_device() != _current():
+        raise ValueError(f"{name} is on {t.device}, the current device is cuda:{_current()}")
+
+
+def _any(t, name, dtypes=_DTYPES):
+    """_dev for a tensor of one of the types `dtypes`, on the current device."""
+    _here(t, name)
     if t.dtype not in dtypes:
         raise TypeError(f"{name} must be one of {', '.join(str(d) for d in dtypes)}, got {t.dtype}")
-    if t.device.index != torch.cuda.current_device():
-        raise ValueError(f"{name} is on {t.device}, the current device is cuda:{torch.cuda.current_device()}")
     if not t.is_contiguous():
         raise ValueError(f"{name} must be contiguous")
     return t
@@ -729,12 +737,9 @@ def flexnorm_bwd(x, weight, grad_out, mean, rstd, layout=BCN, need_x=True, need_
 def _score_dims(t, layout, name):
     """(B, N, C, row stride) of class scores: contiguous, or rows (point-major: a position's; channel-major: a class's) that lie
     evenly spaced, as in a padded vocabulary's first C columns."""
-    if not isinstance(t, torch.Tensor) or not t.is_cuda:
-        raise TypeError(f"{name} must be a CUDA tensor")
+    _here(t, name)
     if t.dtype not in _DTYPES:
         raise TypeError(f"{name} must be fp32, bf16 or fp16, got {t.dtype}")
-    if t.device.index != torch.cuda.current_device():
-        raise ValueError(f"{name} is on {t.device}, the current device is cuda:{torch.cuda.current_device()}")
     if t.dim() != 3:
         raise ValueError(f"{name} must be 3-D")
     B, rows, width = t.shape
@@ -773,7 +778,7 @@ def flexlogp_fwd(logits, target=None, top=0, layout=BCN, workspace=None):
         shape = (B, top, N) if layout == BCN else (B, N, top)
         top_logp = torch.empty(shape, dtype=torch.float32, device=logits.device)
         top_class = torch.empty(shape, dtype=torch.int32, device=logits.device)
-    ws, ws_bytes = _ws_arg(workspace, logits.device, need)
+    ws, ws_bytes = _ws_arg(workspace, logits.device, need) if need > _LOGP_NO_WORKSPACE else (None, 0)
     _check(lib().flexlogp_fwd(_ptr(logits), _ptr(target), _ptr(logp), _ptr(entropy), _ptr(lse), _ptr(top_logp), _ptr(top_class),
                               B, N, C, top, row, _DTYPES[logits.dtype], layout, _ptr(ws), ws_bytes, _stream()), "flexlogp_fwd")
     return logp, entropy, lse, top_logp, top_class
@@ -912,8 +917,7 @@ def flexadamw_step(plan, grads, lr, grad_scale=None):
     if len(grads) != len(counts):
         raise ValueError(f"{len(grads)} gradients for {len(counts)} parameters")
     device = plan._memory.device
-    if device.index != torch.cuda.current_device():
-        raise ValueError(f"the plan is on {device}, the current device is cuda:{torch.cuda.current_device()}")
+    _here(plan._memory, "the plan")
     at = plan._grads
     for i, g in enumerate(grads):
         if g is None:

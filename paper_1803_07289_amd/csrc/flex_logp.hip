@@ -414,13 +414,17 @@ __global__ __launch_bounds__(64) void logp_join_kernel(const T *__restrict__ x, 
     __shared__ int s_count;
     const int lane = threadIdx.x;
     const int64_t row = blockIdx.x;
+    // all that there is to load is asked for at once (an ignored row's parts have left nothing, and nothing comes of it)
     const int t = a.target ? a.target[row] : 0;
-    if (ignored(a, t)) return;
-    const float target_score = lane == 0 && a.target ? to_f32(x[row * a.stride + t]) : 0.f;
-    Sums k = lane < p.parts ? *(const Sums *)((const char *)p.sums + (row * p.parts + lane) * SUMS_BYTES) : Sums{-INFINITY, 0.f, 0.f};
+    Sums k{-INFINITY, 0.f, 0.f};
+    if (lane < p.parts) k = *(const Sums *)((const char *)p.sums + (row * p.parts + lane) * SUMS_BYTES);
     const Candidate *lists = p.best + row * p.parts * a.top;
     const int entries = p.parts * a.top, depth = 64 / p.parts;
-    const Candidate looked_at = lane < depth * p.parts && lane / p.parts < a.top ? lists[lane % p.parts * a.top + lane / p.parts] : 0;
+    Candidate looked_at = 0, first = 0;
+    if (lane < depth * p.parts && lane / p.parts < a.top) looked_at = lists[lane % p.parts * a.top + lane / p.parts];
+    if (lane < entries) first = lists[lane];
+    if (ignored(a, t)) return;
+    const float target_score = lane == 0 && a.target ? to_f32(x[row * a.stride + t]) : 0.f;
     if (lane == 0) s_count = 0;
     const float m = centre(lanes_max<64>(k.m));
     const float d = fmaxf(k.m - m, MASKED), e = __builtin_amdgcn_exp2f(d * LOG2E);
@@ -431,7 +435,7 @@ __global__ __launch_bounds__(64) void logp_join_kernel(const T *__restrict__ x, 
     const float least = reached_by(looked_at ? score_of(looked_at) : -INFINITY, a.top);
     __syncthreads();
     for (int i = lane; i < entries; i += 64) {
-        const Candidate e = lists[i];
+        const Candidate e = i < 64 ? first : lists[i];
         if (e && score_of(e) >= least) s_list[atomicAdd(&s_count, 1)] = e;
     }
     __syncthreads();
@@ -715,10 +719,10 @@ extern "C" {
 size_t flexlogp_fwd_workspace_bytes(int B, int N, int C, int top, int dtype, int layout)
 {
     if (!logp_sizes_ok(B, N, C, layout == FLEX_LAYOUT_BCN ? N : C, dtype, layout) || top < 0 || top > FLEX_LOGP_MAX_TOP || top > C) return 0;
-    if (layout == FLEX_LAYOUT_BCN || C <= row_columns_max(dtype)) return 256;
+    if (layout == FLEX_LAYOUT_BCN || C <= row_columns_max(dtype)) return FLEX_LOGP_NO_WORKSPACE;
     const int64_t rows = (int64_t)B * N;
     const int parts = plan_parts(rows, C, dtype).parts;
-    return parts == 1 ? 256 : parts_sums_bytes(rows, parts) + align256((size_t)rows * parts * top * sizeof(Candidate));
+    return parts == 1 ? FLEX_LOGP_NO_WORKSPACE : parts_sums_bytes(rows, parts) + align256((size_t)rows * parts * top * sizeof(Candidate));
 }
 
 int flexlogp_fwd(const void *logits, const int32_t *target, float *logp, float *entropy, float *lse, float *top_logp,
@@ -728,8 +732,8 @@ int flexlogp_fwd(const void *logits, const int32_t *target, float *logp, float *
     if (!logits || !entropy || !lse || (target == nullptr) != (logp == nullptr)) return FLEX_ERR_NULL;
     if (top > 0 && (!top_logp || !top_class)) return FLEX_ERR_NULL;
     if (!logp_sizes_ok(B, N, C, row_stride, dtype, layout) || top < 0 || top > FLEX_LOGP_MAX_TOP || top > C) return FLEX_ERR_SHAPE;
-    if (!workspace || ((uintptr_t)workspace & 255) || workspace_bytes < flexlogp_fwd_workspace_bytes(B, N, C, top, dtype, layout))
-        return FLEX_ERR_WORKSPACE;
+    const size_t need = flexlogp_fwd_workspace_bytes(B, N, C, top, dtype, layout);
+    if (need > FLEX_LOGP_NO_WORKSPACE && (!workspace || ((uintptr_t)workspace & 255) || workspace_bytes < need)) return FLEX_ERR_WORKSPACE;
     const bool bcn = layout == FLEX_LAYOUT_BCN;
     const LogpArgs a{target, logp, entropy, lse, top_logp, top_class, (int64_t)B * N, row_stride, N, C, top};
     const hipError_t e = with_dtype(dtype, [&](auto t) {

@@ -55,8 +55,8 @@ def logp_fwd(L, x=ONE, t=ONE, lp=ONE, h=ONE, lse=ONE, tl=ONE, tc=ONE, B=1, N=8, 
 @pytest.mark.parametrize("change, status", [
     (dict(x=NONE), 1), (dict(h=NONE), 1), (dict(lse=NONE), 1), (dict(t=NONE), 1), (dict(lp=NONE), 1), (dict(tl=NONE), 1), (dict(tc=NONE), 1),
     (dict(B=0), 2), (dict(C=(1 << 20) + 1, row=BIG), 2), (dict(top=-1), 2), (dict(top=33), 2), (dict(C=1, top=2), 2), (dict(row=63), 2),
-    (dict(row=1 << 31), 2), (dict(layout=0, row=7), 2), (dict(dtype=3), 2), (dict(layout=4), 2), (dict(ws=NONE), 4),
-    (dict(ws=ctypes.c_void_p(8)), 4), (dict(ws_bytes=0), 4)])
+    (dict(row=1 << 31), 2), (dict(layout=0, row=7), 2), (dict(dtype=3), 2), (dict(layout=4), 2), (dict(C=100_000, row=100_000, ws=NONE), 4),
+    (dict(C=100_000, row=100_000, ws=ctypes.c_void_p(8)), 4), (dict(C=100_000, row=100_000, ws_bytes=256), 4)])
 def test_log_probabilities_refuse(L, change, status):
     assert logp_fwd(L, **change) == status
 
