@@ -418,8 +418,9 @@ typedef enum { FLEX_F32 = 0, FLEX_BF16 = 1, FLEX_F16 = 2 } flex_dtype;
  * Layer norm over the C channels of every position:
  *   y = (x - mean) * rstd * weight + bias,  mean over the channels,  rstd = 1 / sqrt(mean((x - mean)^2) + eps)
  * weight / bias [C] in param_dtype (FLEX_F32 or x's type); both NULL: not scaled.  mean / rstd fp32 [B,N] for the backward pass;
- * either may be NULL.  y must not overlap x (y == x is refused).  eps >= 0.
+ * either may be NULL.  y must not overlap x (y == x is refused).  eps >= 0, C <= FLEX_NORM_MAX_CHANNELS.
  */
+#define FLEX_NORM_MAX_CHANNELS (1 << 20)
 int flexnorm_fwd(const void *x, const void *weight, const void *bias, void *y, float *mean, float *rstd,
                  int B, int N, int C, float eps, int dtype, int param_dtype, int layout, void *stream);
 

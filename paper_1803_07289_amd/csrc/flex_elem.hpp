@@ -110,32 +110,12 @@ __device__ __forceinline__ int lanes_min(int v)
     return lanes_reduce<L>(v, [](int a, int b) { return min(a, b); });
 }
 
-// a vector over the channels in a parameter type that is known at run time (read rarely: once a workgroup, or from a cache)
-__device__ __forceinline__ float load_param(const void *p, int dtype, int64_t i)
-{
-    if (dtype == FLEX_F32) return ((const float *)p)[i];
-    if (dtype == FLEX_BF16) return to_f32(((const bf16 *)p)[i]);
-    return to_f32(((const _Float16 *)p)[i]);
-}
+// an element of a vector over the channels in a parameter type that is known at run time
 __device__ __forceinline__ void store_param(void *p, int dtype, int64_t i, float v)
 {
     if (dtype == FLEX_F32) ((float *)p)[i] = v;
     else if (dtype == FLEX_BF16) ((bf16 *)p)[i] = (bf16)v;
     else ((_Float16 *)p)[i] = (_Float16)v;
-}
-
-// sums over the wave, the same on every lane
-__device__ __forceinline__ float wave_sum(float v)
-{
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o);
-    return v;
-}
-__device__ __forceinline__ float wave_max(float v)
-{
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor(v, o));
-    return v;
 }
 
 }  // namespace flex

@@ -2,100 +2,667 @@
 //   y = (x - mean) rstd w + b,  rstd = 1 / sqrt(mean((x - mean)^2) + eps)
 //   with xh = (x - mean) rstd and h = g w:  grad_x = rstd (h - mean(h) - xh mean(h xh)),
 //   grad_w = sum over positions of g xh, grad_b = sum of g.
-// Sums and statistics are fp32; the mean square is taken about the mean (two passes), which loses nothing to cancellation.
+// Sums and statistics are fp32; the mean square is taken about the mean, which loses nothing to cancellation.  Memory bounds all of it:
+// a row is read once and stays in registers (fp32) until it is done; only rows too long for that are read again, from L2.
 #include "flex_elem.hpp"
 #include <algorithm>
 
 namespace flex {
 
-// A wave for each position; channel c of position p of cloud b is x[b * C * N + p * ps + c * cs].
+// A vector over the channels, in the tensor's type or in fp32: columns c .. c + N.
 template <class T>
-__global__ __launch_bounds__(256) void norm_fwd_kernel(const T *__restrict__ x, const void *w, const void *b, T *__restrict__ y,
-                                                       float *mean_out, float *rstd_out, int64_t rows, int N, int C, int64_t ps,
-                                                       int64_t cs, float eps, int pdtype)
+struct Param {
+    const void *p;
+    int f32;
+    __device__ __forceinline__ void load(int c, float (&x)[LANE_ELEMENTS<T>]) const
+    {
+        constexpr int N = LANE_ELEMENTS<T>;
+        if (sizeof(T) == 4 || f32) Chunk<float, N>::load((const float *)p + c, x);
+        else Chunk<T>::load((const T *)p + c, x);
+    }
+    __device__ __forceinline__ float operator[](int c) const { return sizeof(T) == 4 || f32 ? ((const float *)p)[c] : to_f32(((const T *)p)[c]); }
+};
+
+// Sum over the L threads that share a row: lanes of a wave, or a workgroup of L = 256 or 1024 through LDS (`place`: a slot of its own for
+// each sum between two barriers of the caller).
+template <int L>
+__device__ __forceinline__ float row_sum(float v, float *place)
 {
-    const int lane = threadIdx.x & 63;
-    const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-    if (row >= rows) return;
-    const int64_t base = row / N * ((int64_t)N * C) + row % N * ps;
-    float sum = 0.f;
-    for (int c = lane; c < C; c += 64) sum += to_f32(x[base + c * cs]);
-    const float mean = wave_sum(sum) / (float)C;
-    float sq = 0.f;
-    for (int c = lane; c < C; c += 64) {
-        const float d = to_f32(x[base + c * cs]) - mean;
+    if (L <= 64) return lanes_sum<L <= 64 ? L : 64>(v);
+    v = lanes_sum<64>(v);
+    if ((threadIdx.x & 63) == 0) place[threadIdx.x >> 6] = v;
+    __syncthreads();
+    v = place[0];
+#pragma unroll
+    for (int i = 1; i < L / 64; ++i) v += place[i];
+    return v;
+}
+
+// ---- point-major ------------------------------------------------------------------------------------------------------------
+// L threads hold a row, U times 16 bytes each; a group of them takes R rows, which it asks for together.  NARROW: rows of fewer
+// channels than 16 bytes hold.
+template <class T, int L, int U, int R, bool NARROW>
+__global__ __launch_bounds__(L > 256 ? L : 256) void norm_rows_kernel(const T *__restrict__ x, Param<T> w, Param<T> b, T *__restrict__ y,
+                                                                      float *mean_out, float *rstd_out, int64_t rows, int C, float eps)
+{
+    constexpr int N = LANE_ELEMENTS<T>, WG = L > 256 ? L : 256, G = WG / L;
+    __shared__ float s_place[2 * R][WG / 64];
+    const int sub = threadIdx.x % L;
+    const int64_t row0 = (int64_t)blockIdx.x * (G * R) + threadIdx.x / L;
+    float v[R][U][N];
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        const int64_t row = min(row0 + r * G, rows - 1);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int c0 = (u * L + sub) * N;
+            if (NARROW) {
+#pragma unroll
+                for (int j = 0; j < N; ++j) v[r][u][j] = c0 + j < C ? to_f32(x[row * C + c0 + j]) : 0.f;
+            } else
+                Chunk<T>::load(x + row * C + Chunk<T>::from(c0, C), v[r][u]);
+        }
+    }
+    const float count = (float)C;
+    float mean[R], rstd[R];
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        float sum = 0.f;
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (!NARROW) Chunk<T>::mask(v[r][u], (u * L + sub) * N, C, 0.f);
+#pragma unroll
+            for (int j = 0; j < N; ++j) sum += v[r][u][j];
+        }
+        mean[r] = row_sum<L>(sum, s_place[2 * r]) / count;
+    }
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        float sq = 0.f;
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int c0 = (u * L + sub) * N;
+            float d[N];
+#pragma unroll
+            for (int j = 0; j < N; ++j) d[j] = v[r][u][j] - mean[r];
+            if (NARROW) {
+#pragma unroll
+                for (int j = 0; j < N; ++j) d[j] = c0 + j < C ? d[j] : 0.f;
+            } else
+                Chunk<T>::mask(d, c0, C, 0.f);
+#pragma unroll
+            for (int j = 0; j < N; ++j) sq += d[j] * d[j];
+        }
+        rstd[r] = 1.f / sqrtf(row_sum<L>(sq, s_place[2 * r + 1]) / count + eps);
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        const int c0 = (u * L + sub) * N;
+        if (c0 >= C) break;
+        const int from = NARROW ? c0 : Chunk<T>::from(c0, C);
+        float ww[N], bb[N];
+        if (w.p) {
+            if (NARROW) {
+#pragma unroll
+                for (int j = 0; j < N; ++j) {
+                    ww[j] = c0 + j < C ? w[c0 + j] : 0.f;
+                    bb[j] = c0 + j < C ? b[c0 + j] : 0.f;
+                }
+            } else {
+                w.load(from, ww);
+                b.load(from, bb);
+            }
+        }
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            const int64_t row = row0 + r * G;
+            if (row >= rows) break;
+            float out[N];
+#pragma unroll
+            for (int j = 0; j < N; ++j) {
+                out[j] = (v[r][u][j] - mean[r]) * rstd[r];
+                if (w.p) out[j] = out[j] * ww[j] + bb[j];
+            }
+            T *to = y + row * C + c0;
+            if (c0 + N <= C) Chunk<T>::store(to, out);
+            else
+#pragma unroll
+                for (int j = 0; j < N; ++j)
+                    if (from + j >= c0 && from + j < C) y[row * C + from + j] = (T)out[j];
+        }
+    }
+    if (sub == 0)
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            const int64_t row = row0 + r * G;
+            if (row >= rows) break;
+            if (mean_out) mean_out[row] = mean[r];
+            if (rstd_out) rstd_out[row] = rstd[r];
+        }
+}
+
+// Rows of any length, a workgroup to each, read three times.
+template <class T>
+__global__ __launch_bounds__(1024) void norm_long_rows_kernel(const T *__restrict__ x, Param<T> w, Param<T> b, T *__restrict__ y,
+                                                              float *mean_out, float *rstd_out, int C, float eps)
+{
+    __shared__ float s_place[2][16];
+    const int64_t row = blockIdx.x;
+    const T *at = x + row * C;
+    const float count = (float)C;
+    float sum = 0.f, sq = 0.f;
+    for (int c = threadIdx.x; c < C; c += 1024) sum += to_f32(at[c]);
+    const float mean = row_sum<1024>(sum, s_place[0]) / count;
+    for (int c = threadIdx.x; c < C; c += 1024) {
+        const float d = to_f32(at[c]) - mean;
         sq += d * d;
     }
-    const float rstd = 1.f / sqrtf(wave_sum(sq) / (float)C + eps);
-    for (int c = lane; c < C; c += 64) {
-        const float v = (to_f32(x[base + c * cs]) - mean) * rstd;
-        y[base + c * cs] = (T)(w ? v * load_param(w, pdtype, c) + load_param(b, pdtype, c) : v);
+    const float rstd = 1.f / sqrtf(row_sum<1024>(sq, s_place[1]) / count + eps);
+    for (int c = threadIdx.x; c < C; c += 1024) {
+        const float d = (to_f32(at[c]) - mean) * rstd;
+        y[row * C + c] = (T)(w.p ? d * w[c] + b[c] : d);
     }
-    if (lane == 0) {
+    if (threadIdx.x == 0) {
         if (mean_out) mean_out[row] = mean;
         if (rstd_out) rstd_out[row] = rstd;
     }
 }
 
-template <class T>
-__global__ __launch_bounds__(256) void norm_bwd_kernel(const T *__restrict__ x, const void *w, const T *__restrict__ g,
-                                                       const float *mean, const float *rstd, T *__restrict__ gx, int64_t rows,
-                                                       int N, int C, int64_t ps, int64_t cs, int pdtype)
+// Backward: a group of L threads walks over rows, its own columns' shares of grad_w and grad_b in registers, which the groups of a
+// workgroup add up in LDS at the end: one partial sum of 2 C a workgroup.
+// PARAMS: with grad_w and grad_b (gx may be null then); otherwise only gx.
+template <class T, int L, int U, bool PARAMS, bool NARROW>
+__global__ __launch_bounds__(L > 256 ? L : 256) void norm_rows_bwd_kernel(const T *__restrict__ x, Param<T> w, const T *__restrict__ g,
+                                                                          const float *__restrict__ mean, const float *__restrict__ rstd,
+                                                                          T *__restrict__ gx, float *__restrict__ partials,
+                                                                          int64_t rows, int C)
 {
-    const int lane = threadIdx.x & 63;
-    const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-    if (row >= rows) return;
-    const int64_t base = row / N * ((int64_t)N * C) + row % N * ps;
-    const float m = mean[row], r = rstd[row];
-    float s1 = 0.f, s2 = 0.f;
-    for (int c = lane; c < C; c += 64) {
-        const float h = to_f32(g[base + c * cs]) * (w ? load_param(w, pdtype, c) : 1.f);
-        s1 += h;
-        s2 += h * ((to_f32(x[base + c * cs]) - m) * r);
+    constexpr int N = LANE_ELEMENTS<T>, WG = L > 256 ? L : 256, G = WG / L;
+    __shared__ float s_place[2][2][WG / 64];
+    const int sub = threadIdx.x % L, group = threadIdx.x / L;
+    const float count = (float)C;
+    float ww[U][N], gw[U][N], gb[U][N];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        const int c0 = (u * L + sub) * N;
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+            ww[u][j] = 1.f;
+            gw[u][j] = gb[u][j] = 0.f;
+        }
+        if (w.p) {
+            if (NARROW) {
+#pragma unroll
+                for (int j = 0; j < N; ++j) ww[u][j] = c0 + j < C ? w[c0 + j] : 0.f;
+            } else
+                w.load(Chunk<T>::from(c0, C), ww[u]);
+        }
     }
-    s1 = wave_sum(s1) / (float)C;
-    s2 = wave_sum(s2) / (float)C;
-    for (int c = lane; c < C; c += 64) {
-        const float h = to_f32(g[base + c * cs]) * (w ? load_param(w, pdtype, c) : 1.f);
-        gx[base + c * cs] = (T)((h - s1 - (to_f32(x[base + c * cs]) - m) * r * s2) * r);
+    const int64_t step = (int64_t)gridDim.x * G;
+    int turn = 0;
+    // (a workgroup's groups take as many turns as each other: lanes and barriers stay together)
+    for (int64_t first = (int64_t)blockIdx.x * G; first < rows; first += step, turn ^= 1) {
+        const int64_t row = min(first + group, rows - 1);
+        const bool mine = first + group < rows;
+        float xh[U][N], gg[U][N];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int c0 = (u * L + sub) * N;
+            if (NARROW) {
+#pragma unroll
+                for (int j = 0; j < N; ++j) {
+                    xh[u][j] = c0 + j < C ? to_f32(x[row * C + c0 + j]) : 0.f;
+                    gg[u][j] = c0 + j < C ? to_f32(g[row * C + c0 + j]) : 0.f;
+                }
+            } else {
+                Chunk<T>::load(x + row * C + Chunk<T>::from(c0, C), xh[u]);
+                Chunk<T>::load(g + row * C + Chunk<T>::from(c0, C), gg[u]);
+            }
+        }
+        const float m = mean[row], r = rstd[row];
+        float s1 = 0.f, s2 = 0.f;
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (!NARROW) Chunk<T>::mask(gg[u], (u * L + sub) * N, C, 0.f);
+#pragma unroll
+            for (int j = 0; j < N; ++j) {
+                xh[u][j] = (xh[u][j] - m) * r;
+                const float h = gg[u][j] * ww[u][j];
+                s1 += h;
+                s2 += h * xh[u][j];
+                if (PARAMS && mine) {
+                    gw[u][j] += gg[u][j] * xh[u][j];
+                    gb[u][j] += gg[u][j];
+                }
+            }
+        }
+        if (PARAMS && !gx) continue;
+        s1 = row_sum<L>(s1, s_place[turn][0]) / count;
+        s2 = row_sum<L>(s2, s_place[turn][1]) / count;
+        if (!mine) continue;
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int c0 = (u * L + sub) * N;
+            if (c0 >= C) break;
+            float out[N];
+#pragma unroll
+            for (int j = 0; j < N; ++j) out[j] = (gg[u][j] * ww[u][j] - s1 - xh[u][j] * s2) * r;
+            T *to = gx + row * C;
+            if (c0 + N <= C) Chunk<T>::store(to + c0, out);
+            else {
+                const int from = NARROW ? c0 : Chunk<T>::from(c0, C);
+#pragma unroll
+                for (int j = 0; j < N; ++j)
+                    if (from + j >= c0 && from + j < C) to[from + j] = (T)out[j];
+            }
+        }
+    }
+    if (!PARAMS) return;
+    // (each group's columns begin at c0; what a clamped lane holds before that is zero, its gradient having been masked)
+    __shared__ float s_sum[L < 256 ? 2 * 256 * U * N : 1];
+    float *const to = partials + (int64_t)blockIdx.x * 2 * C;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        const int c0 = (u * L + sub) * N, from = NARROW ? c0 : Chunk<T>::from(c0, C);
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+            if (L < 256) {
+                s_sum[((group * U + u) * N + j) * L + sub] = gw[u][j];
+                s_sum[((group * U + u) * N + j) * L + sub + 256 * U * N] = gb[u][j];
+            } else if (from + j >= c0 && from + j < C) {
+                to[from + j] = gw[u][j];
+                to[C + from + j] = gb[u][j];
+            }
+        }
+    }
+    if (L >= 256) return;
+    __syncthreads();
+    for (int i = threadIdx.x; i < 2 * L * U * N; i += 256) {
+        const int which = i / (L * U * N), at = i % (L * U * N);
+        float sum = 0.f;
+#pragma unroll
+        for (int k = 0; k < G; ++k) sum += s_sum[which * 256 * U * N + k * (U * N * L) + at];
+        const int lane = at % L, j = at / L % N, u = at / L / N;
+        const int c0 = (u * L + lane) * N, from = NARROW ? c0 : Chunk<T>::from(c0, C);
+        if (from + j >= c0 && from + j < C) to[which * C + from + j] = sum;
     }
 }
 
-// partials[slice][0 | 1][C]: a thread sums one channel over its slice of positions
 template <class T>
-__global__ __launch_bounds__(256) void norm_params_kernel(const T *__restrict__ x, const T *__restrict__ g, const float *mean,
-                                                          const float *rstd, float *partials, int64_t rows, int64_t per, int N,
-                                                          int C, int64_t ps, int64_t cs)
+__global__ __launch_bounds__(1024) void norm_long_rows_bwd_kernel(const T *__restrict__ x, Param<T> w, const T *__restrict__ g,
+                                                                  const float *__restrict__ mean, const float *__restrict__ rstd,
+                                                                  T *__restrict__ gx, int C)
+{
+    __shared__ float s_place[2][16];
+    const int64_t row = blockIdx.x;
+    const float count = (float)C, m = mean[row], r = rstd[row];
+    float s1 = 0.f, s2 = 0.f;
+    for (int c = threadIdx.x; c < C; c += 1024) {
+        const float h = to_f32(g[row * C + c]) * (w.p ? w[c] : 1.f);
+        s1 += h;
+        s2 += h * ((to_f32(x[row * C + c]) - m) * r);
+    }
+    s1 = row_sum<1024>(s1, s_place[0]) / count;
+    s2 = row_sum<1024>(s2, s_place[1]) / count;
+    for (int c = threadIdx.x; c < C; c += 1024) {
+        const float h = to_f32(g[row * C + c]) * (w.p ? w[c] : 1.f);
+        gx[row * C + c] = (T)((h - s1 - (to_f32(x[row * C + c]) - m) * r * s2) * r);
+    }
+}
+
+// Parameters' partial sums of long rows: a thread to a channel, a slice of the positions to a row of workgroups.
+template <class T>
+__global__ __launch_bounds__(256) void norm_long_rows_params_kernel(const T *__restrict__ x, const T *__restrict__ g,
+                                                                    const float *__restrict__ mean, const float *__restrict__ rstd,
+                                                                    float *__restrict__ partials, int64_t rows, int64_t per, int C)
 {
     const int c = blockIdx.x * 256 + threadIdx.x;
     if (c >= C) return;
     float gw = 0.f, gb = 0.f;
     const int64_t end = min(rows, (int64_t)(blockIdx.y + 1) * per);
     for (int64_t row = (int64_t)blockIdx.y * per; row < end; ++row) {
-        const int64_t at = row / N * ((int64_t)N * C) + row % N * ps + c * cs;
-        const float v = to_f32(g[at]);
-        gw += v * ((to_f32(x[at]) - mean[row]) * rstd[row]);
+        const float v = to_f32(g[row * C + c]);
+        gw += v * ((to_f32(x[row * C + c]) - mean[row]) * rstd[row]);
         gb += v;
     }
     partials[((int64_t)blockIdx.y * 2 + 0) * C + c] = gw;
     partials[((int64_t)blockIdx.y * 2 + 1) * C + c] = gb;
 }
 
-__global__ __launch_bounds__(256) void norm_params_sum_kernel(const float *__restrict__ partials, int slices, void *gw, void *gb,
-                                                              int C, int pdtype)
+// ---- channel-major ----------------------------------------------------------------------------------------------------------
+// A lane to a position, W waves of a workgroup share the channels: R of them a wave in registers, or (R = 0) any number, read again.
+constexpr int COL_CHANNELS = 16;
+
+// sums over the waves of a workgroup, by position
+template <int W>
+__device__ __forceinline__ float waves_sum(float v, float (*place)[64])
 {
-    const int c = blockIdx.x * 256 + threadIdx.x;
-    if (c >= C) return;
-    float a = 0.f, b = 0.f;
-    for (int i = 0; i < slices; ++i) {
-        a += partials[((int64_t)i * 2 + 0) * C + c];
-        b += partials[((int64_t)i * 2 + 1) * C + c];
-    }
-    store_param(gw, pdtype, c, a);
-    store_param(gb, pdtype, c, b);
+    if (W == 1) return v;
+    const int lane = threadIdx.x & 63;
+    place[threadIdx.x >> 6][lane] = v;
+    __syncthreads();
+    v = place[0][lane];
+#pragma unroll
+    for (int i = 1; i < W; ++i) v += place[i][lane];
+    return v;
 }
 
-static int norm_slices(int64_t rows) { return (int)std::min<int64_t>(256, cdiv64(rows, 64)); }
+template <class T, int W, int R>
+__global__ __launch_bounds__(64 * W) void norm_cols_kernel(const T *__restrict__ x, Param<T> w, Param<T> b, T *__restrict__ y,
+                                                           float *mean_out, float *rstd_out, int N, int C, float eps)
+{
+    __shared__ float s_place[2][W][64];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const unsigned tiles = (unsigned)(N + 63) / 64;
+    const int64_t cloud = blockIdx.x / tiles;
+    const int n = (int)(blockIdx.x % tiles) * 64 + lane;
+    const bool mine = n < N;
+    const int per = R ? R : (C + W - 1) / W, first = wave * per, last = min(first + per, C);
+    const int64_t base = cloud * C * (int64_t)N + min(n, N - 1);
+    const float count = (float)C;
+    float v[R ? R : 1], sum = 0.f, sq = 0.f;
+    if (R) {
+#pragma unroll
+        for (int i = 0; i < R; ++i) v[i] = first + i < last ? to_f32(x[base + (int64_t)(first + i) * N]) : 0.f;
+#pragma unroll
+        for (int i = 0; i < R; ++i) sum += v[i];
+    } else
+        for (int c = first; c < last; ++c) sum += to_f32(x[base + (int64_t)c * N]);
+    const float mean = waves_sum<W>(sum, s_place[0]) / count;
+    if (R) {
+#pragma unroll
+        for (int i = 0; i < R; ++i) {
+            const float d = v[i] - mean;
+            if (first + i < last) sq += d * d;
+        }
+    } else
+        for (int c = first; c < last; ++c) {
+            const float d = to_f32(x[base + (int64_t)c * N]) - mean;
+            sq += d * d;
+        }
+    const float rstd = 1.f / sqrtf(waves_sum<W>(sq, s_place[1]) / count + eps);
+    if (!mine) return;
+    auto put = [&](int c, float value) {
+        const float d = (value - mean) * rstd;
+        y[base + (int64_t)c * N] = (T)(w.p ? d * w[c] + b[c] : d);
+    };
+    if (R) {
+#pragma unroll
+        for (int i = 0; i < R; ++i)
+            if (first + i < last) put(first + i, v[i]);
+    } else
+        for (int c = first; c < last; ++c) put(c, to_f32(x[base + (int64_t)c * N]));
+    if (wave == 0) {
+        if (mean_out) mean_out[cloud * N + n] = mean;
+        if (rstd_out) rstd_out[cloud * N + n] = rstd;
+    }
+}
+
+// Backward: a workgroup walks over tiles of 64 positions; a lane adds its positions' shares of grad_w and grad_b up for each of its
+// channels, the lanes of a wave meet at the end.
+template <class T, int W, bool PARAMS>
+__global__ __launch_bounds__(64 * W) void norm_cols_bwd_kernel(const T *__restrict__ x, Param<T> w, const T *__restrict__ g,
+                                                               const float *__restrict__ mean, const float *__restrict__ rstd,
+                                                               T *__restrict__ gx, float *__restrict__ partials, int N, int C,
+                                                               unsigned tiles, unsigned total)
+{
+    constexpr int R = COL_CHANNELS;
+    __shared__ float s_place[2][2][W][64];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int first = wave * R, many = min(R, C - first);
+    const float count = (float)C;
+    float gw[R], gb[R];
+#pragma unroll
+    for (int i = 0; i < R; ++i) gw[i] = gb[i] = 0.f;
+    int turn = 0;
+    for (unsigned tile = blockIdx.x; tile < total; tile += gridDim.x, turn ^= 1) {
+        const int64_t cloud = tile / tiles;
+        const int n = (int)(tile % tiles) * 64 + lane;
+        const bool mine = n < N;
+        const int64_t base = (cloud * C + first) * (int64_t)N + min(n, N - 1), at = cloud * N + min(n, N - 1);
+        float xh[R], gg[R], s1 = 0.f, s2 = 0.f;
+#pragma unroll
+        for (int i = 0; i < R; ++i) {
+            xh[i] = i < many ? to_f32(x[base + (int64_t)i * N]) : 0.f;
+            gg[i] = i < many && mine ? to_f32(g[base + (int64_t)i * N]) : 0.f;
+        }
+        const float m = mean[at], r = rstd[at];
+#pragma unroll
+        for (int i = 0; i < R; ++i) {
+            xh[i] = (xh[i] - m) * r;
+            const float h = i < many && w.p ? gg[i] * w[first + i] : gg[i];
+            s1 += h;
+            s2 += h * xh[i];
+            if (PARAMS) {
+                gw[i] += gg[i] * xh[i];
+                gb[i] += gg[i];
+            }
+        }
+        if (PARAMS && !gx) continue;
+        s1 = waves_sum<W>(s1, s_place[turn][0]) / count;
+        s2 = waves_sum<W>(s2, s_place[turn][1]) / count;
+        if (!mine) continue;
+#pragma unroll
+        for (int i = 0; i < R; ++i)
+            if (i < many) {
+                const float h = w.p ? gg[i] * w[first + i] : gg[i];
+                gx[base + (int64_t)i * N] = (T)((h - s1 - xh[i] * s2) * r);
+            }
+    }
+    if (!PARAMS) return;
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+        const float a = lanes_sum<64>(gw[i]), b = lanes_sum<64>(gb[i]);
+        if (i < many && lane == i) {
+            partials[(int64_t)blockIdx.x * 2 * C + first + i] = a;
+            partials[(int64_t)blockIdx.x * 2 * C + C + first + i] = b;
+        }
+    }
+}
+
+// more channels than the waves hold: read twice
+template <class T>
+__global__ __launch_bounds__(1024) void norm_many_cols_bwd_kernel(const T *__restrict__ x, Param<T> w, const T *__restrict__ g,
+                                                                  const float *__restrict__ mean, const float *__restrict__ rstd,
+                                                                  T *__restrict__ gx, int N, int C)
+{
+    constexpr int W = 16;
+    __shared__ float s_place[2][W][64];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const unsigned tiles = (unsigned)(N + 63) / 64;
+    const int64_t cloud = blockIdx.x / tiles;
+    const int n = (int)(blockIdx.x % tiles) * 64 + lane;
+    const int per = (C + W - 1) / W, first = wave * per, last = min(first + per, C);
+    const int64_t base = cloud * C * (int64_t)N + min(n, N - 1), at = cloud * N + min(n, N - 1);
+    const float m = mean[at], r = rstd[at], count = (float)C;
+    float s1 = 0.f, s2 = 0.f;
+    for (int c = first; c < last; ++c) {
+        const float h = to_f32(g[base + (int64_t)c * N]) * (w.p ? w[c] : 1.f);
+        s1 += h;
+        s2 += h * ((to_f32(x[base + (int64_t)c * N]) - m) * r);
+    }
+    s1 = waves_sum<W>(s1, s_place[0]) / count;
+    s2 = waves_sum<W>(s2, s_place[1]) / count;
+    if (n >= N) return;
+    for (int c = first; c < last; ++c) {
+        const float h = to_f32(g[base + (int64_t)c * N]) * (w.p ? w[c] : 1.f);
+        gx[base + (int64_t)c * N] = (T)((h - s1 - (to_f32(x[base + (int64_t)c * N]) - m) * r * s2) * r);
+    }
+}
+
+// their parameters' partial sums: a workgroup to a channel and a slice of the positions
+template <class T>
+__global__ __launch_bounds__(256) void norm_many_cols_params_kernel(const T *__restrict__ x, const T *__restrict__ g,
+                                                                    const float *__restrict__ mean, const float *__restrict__ rstd,
+                                                                    float *__restrict__ partials, int64_t rows, int64_t per, int N, int C)
+{
+    __shared__ float s_place[2][4];
+    const int c = blockIdx.x;
+    const int64_t end = min(rows, (int64_t)(blockIdx.y + 1) * per);
+    float gw = 0.f, gb = 0.f;
+    for (int64_t row = (int64_t)blockIdx.y * per + threadIdx.x; row < end; row += 256) {
+        const int64_t at = (row / N * C + c) * N + row % N;
+        const float v = to_f32(g[at]);
+        gw += v * ((to_f32(x[at]) - mean[row]) * rstd[row]);
+        gb += v;
+    }
+    gw = row_sum<256>(gw, s_place[0]);
+    gb = row_sum<256>(gb, s_place[1]);
+    if (threadIdx.x == 0) {
+        partials[((int64_t)blockIdx.y * 2 + 0) * C + c] = gw;
+        partials[((int64_t)blockIdx.y * 2 + 1) * C + c] = gb;
+    }
+}
+
+// ---- partial sums to gradients ------------------------------------------------------------------------------------------------
+// 16 columns to a workgroup, 16 threads to a column, in the same order at every call.
+__global__ __launch_bounds__(256) void norm_params_sum_kernel(const float *__restrict__ partials, int slices, void *gw, void *gb, int C,
+                                                              int pdtype)
+{
+    __shared__ float s_sum[16][17];
+    const int column = blockIdx.x * 16 + (threadIdx.x & 15), slot = threadIdx.x >> 4;
+    float sum = 0.f;
+    if (column < 2 * C)
+#pragma unroll 8
+        for (int i = slot; i < slices; i += 16) sum += partials[(int64_t)i * 2 * C + column];
+    s_sum[slot][threadIdx.x & 15] = sum;
+    __syncthreads();
+    if (slot != 0 || column >= 2 * C) return;
+    sum = s_sum[0][threadIdx.x];
+#pragma unroll
+    for (int i = 1; i < 16; ++i) sum += s_sum[i][threadIdx.x];
+    if (column < C) store_param(gw, pdtype, column, sum);
+    else store_param(gb, pdtype, column - C, sum);
+}
+
+// ---- launches -----------------------------------------------------------------------------------------------------------------
+
+// The row kernels' threads and 16-byte pieces: the smallest that hold C.  f(L, U); false: none.
+template <class T, class F>
+static bool with_row_threads(int C, F f)
+{
+    constexpr int N = LANE_ELEMENTS<T>;
+#define FLEX_ROW_THREADS(L, U) \
+    if (C <= L * U * N) return f(std::integral_constant<int, L>{}, std::integral_constant<int, U>{}), true;
+    FLEX_ROW_THREADS(4, 1)
+    FLEX_ROW_THREADS(8, 1)
+    FLEX_ROW_THREADS(16, 1)
+    FLEX_ROW_THREADS(32, 1)
+    FLEX_ROW_THREADS(64, 1)
+    FLEX_ROW_THREADS(64, 2)
+    FLEX_ROW_THREADS(256, 1)
+    FLEX_ROW_THREADS(256, 2)
+    FLEX_ROW_THREADS(256, 4)
+    FLEX_ROW_THREADS(1024, 2)
+    if constexpr (N == 4) FLEX_ROW_THREADS(1024, 4)
+#undef FLEX_ROW_THREADS
+    return false;
+}
+// The longest rows that those hold: 1024 threads, 16 elements each.
+constexpr int ROW_CHANNELS_MAX = 16384, COL_CHANNELS_MAX = 16 * COL_CHANNELS;
+
+// f(W): the waves that hold C channels, channel-major
+template <class F>
+static void with_col_waves(int C, F f)
+{
+    if (C <= COL_CHANNELS) f(std::integral_constant<int, 1>{});
+    else if (C <= 2 * COL_CHANNELS) f(std::integral_constant<int, 2>{});
+    else if (C <= 4 * COL_CHANNELS) f(std::integral_constant<int, 4>{});
+    else if (C <= 8 * COL_CHANNELS) f(std::integral_constant<int, 8>{});
+    else f(std::integral_constant<int, 16>{});
+}
+
+// Partial sums of grad_w and grad_b: the workgroups that walk over the positions, at least four turns to each.
+static int norm_slices(int B, int N, int C, int dtype, bool bcn)
+{
+    const int64_t rows = (int64_t)B * N, cus = device_cu_count();
+    if (bcn) {
+        if (C > COL_CHANNELS_MAX) return (int)std::min<int64_t>(64, cdiv64(rows, 4096));
+        const int64_t waves = cdiv64(C, COL_CHANNELS);
+        return (int)std::min<int64_t>(B * cdiv64(N, 64), std::max<int64_t>(cus, 8 * cus / waves));
+    }
+    if (C > ROW_CHANNELS_MAX) return (int)std::min<int64_t>(64, cdiv64(rows, 16));
+    const int lane = 16 / (int)dtype_bytes(dtype);
+    int64_t groups = 1;
+    for (const int L : {4, 8, 16, 32, 64}) if (C <= L * lane || (L == 64 && C <= 128 * lane)) { groups = 256 / L; break; }
+    return (int)std::max<int64_t>(1, std::min<int64_t>(cdiv64(rows, 4 * groups), groups > 1 ? 4 * cus : 2 * cus));
+}
+
+template <class T>
+static hipError_t launch_norm_fwd(const T *x, const void *weight, const void *bias, T *y, float *mean, float *rstd, int B, int N,
+                                  int C, float eps, int pdtype, bool bcn, hipStream_t s)
+{
+    const int64_t rows = (int64_t)B * N;
+    const Param<T> w{weight, pdtype == FLEX_F32}, b{bias, pdtype == FLEX_F32};
+    if (bcn) {
+        const dim3 grid((unsigned)(B * cdiv64(N, 64)));
+        if (C > COL_CHANNELS_MAX)
+            hipLaunchKernelGGL((norm_cols_kernel<T, 16, 0>), grid, dim3(1024), 0, s, x, w, b, y, mean, rstd, N, C, eps);
+        else
+            with_col_waves(C, [&](auto waves) {
+                constexpr int W = decltype(waves)::value;
+                hipLaunchKernelGGL((norm_cols_kernel<T, W, COL_CHANNELS>), grid, dim3(64 * W), 0, s, x, w, b, y, mean, rstd, N, C, eps);
+            });
+        return hipGetLastError();
+    }
+    if (!with_row_threads<T>(C, [&](auto l, auto u) {
+            constexpr int L = decltype(l)::value, U = decltype(u)::value, R = L <= 64 && U == 1 ? 4 : L == 64 ? 2 : 1;
+            const dim3 grid((unsigned)cdiv64(rows, (int64_t)std::max(256 / L, 1) * R)), wg(std::max(L, 256));
+            if constexpr (L == 4)
+                if (C < LANE_ELEMENTS<T>) {
+                    hipLaunchKernelGGL((norm_rows_kernel<T, L, U, R, true>), grid, wg, 0, s, x, w, b, y, mean, rstd, rows, C, eps);
+                    return;
+                }
+            hipLaunchKernelGGL((norm_rows_kernel<T, L, U, R, false>), grid, wg, 0, s, x, w, b, y, mean, rstd, rows, C, eps);
+        }))
+        hipLaunchKernelGGL(norm_long_rows_kernel<T>, dim3((unsigned)rows), dim3(1024), 0, s, x, w, b, y, mean, rstd, C, eps);
+    return hipGetLastError();
+}
+
+template <class T>
+static hipError_t launch_norm_bwd(const T *x, const void *weight, const T *g, const float *mean, const float *rstd, T *gx, void *gw,
+                                  void *gb, int B, int N, int C, int dtype, int pdtype, bool bcn, float *partials, hipStream_t s)
+{
+    const int64_t rows = (int64_t)B * N;
+    const Param<T> w{weight, pdtype == FLEX_F32};
+    const int slices = norm_slices(B, N, C, dtype, bcn);
+    if (bcn && C <= COL_CHANNELS_MAX) {
+        const unsigned tiles = (unsigned)(N + 63) / 64, total = (unsigned)B * tiles;
+        with_col_waves(C, [&](auto waves) {
+            constexpr int W = decltype(waves)::value;
+            if (gw) hipLaunchKernelGGL((norm_cols_bwd_kernel<T, W, true>), dim3((unsigned)slices), dim3(64 * W), 0, s, x, w, g, mean, rstd, gx, partials, N, C, tiles, total);
+            else hipLaunchKernelGGL((norm_cols_bwd_kernel<T, W, false>), dim3(total), dim3(64 * W), 0, s, x, w, g, mean, rstd, gx, partials, N, C, tiles, total);
+        });
+    } else if (bcn) {
+        if (gx) hipLaunchKernelGGL(norm_many_cols_bwd_kernel<T>, dim3((unsigned)(B * cdiv64(N, 64))), dim3(1024), 0, s, x, w, g, mean, rstd, gx, N, C);
+        if (gw)
+            hipLaunchKernelGGL(norm_many_cols_params_kernel<T>, dim3((unsigned)C, (unsigned)slices), dim3(256), 0, s, x, g, mean, rstd,
+                               partials, rows, cdiv64(rows, slices), N, C);
+    } else if (!with_row_threads<T>(C, [&](auto l, auto u) {
+                   constexpr int L = decltype(l)::value, U = decltype(u)::value;
+                   const dim3 wg(std::max(L, 256)), grid((unsigned)(gw ? slices : cdiv64(rows, std::max(256 / L, 1))));
+                   auto launch = [&](auto params, auto narrow) {
+                       hipLaunchKernelGGL((norm_rows_bwd_kernel<T, L, U, decltype(params)::value, decltype(narrow)::value>), grid, wg, 0, s, x,
+                                          w, g, mean, rstd, gx, partials, rows, C);
+                   };
+                   if constexpr (L == 4)
+                       if (C < LANE_ELEMENTS<T>) {
+                           if (gw) launch(std::true_type{}, std::true_type{});
+                           else launch(std::false_type{}, std::true_type{});
+                           return;
+                       }
+                   if (gw) launch(std::true_type{}, std::false_type{});
+                   else launch(std::false_type{}, std::false_type{});
+               })) {
+        if (gx) hipLaunchKernelGGL(norm_long_rows_bwd_kernel<T>, dim3((unsigned)rows), dim3(1024), 0, s, x, w, g, mean, rstd, gx, C);
+        if (gw)
+            hipLaunchKernelGGL(norm_long_rows_params_kernel<T>, dim3((unsigned)((C + 255) / 256), (unsigned)slices), dim3(256), 0, s, x, g,
+                               mean, rstd, partials, rows, cdiv64(rows, slices), C);
+    }
+    if (gw)
+        hipLaunchKernelGGL(norm_params_sum_kernel, dim3((unsigned)((2 * (int64_t)C + 15) / 16)), dim3(256), 0, s, partials, slices, gw, gb, C, pdtype);
+    return hipGetLastError();
+}
 
 }  // namespace flex
 
@@ -103,8 +670,8 @@ using namespace flex;
 
 static bool norm_sizes_ok(int B, int N, int C, int layout, int dtype, int param_dtype)
 {
-    return B > 0 && N > 0 && C > 0 && (int64_t)B * N < ((int64_t)1 << 31) && (layout == FLEX_LAYOUT_BCN || layout == FLEX_LAYOUT_BNC) &&
-           dtype_ok(dtype) && (param_dtype == FLEX_F32 || param_dtype == dtype);
+    return B > 0 && N > 0 && C > 0 && C <= FLEX_NORM_MAX_CHANNELS && (int64_t)B * N < ((int64_t)1 << 31) &&
+           (layout == FLEX_LAYOUT_BCN || layout == FLEX_LAYOUT_BNC) && dtype_ok(dtype) && (param_dtype == FLEX_F32 || param_dtype == dtype);
 }
 
 extern "C" {
@@ -114,12 +681,10 @@ int flexnorm_fwd(const void *x, const void *weight, const void *bias, void *y, f
 {
     if (!x || !y || (weight == nullptr) != (bias == nullptr)) return FLEX_ERR_NULL;
     if (!norm_sizes_ok(B, N, C, layout, dtype, param_dtype) || !(eps >= 0.f) || x == y) return FLEX_ERR_SHAPE;
-    const int64_t rows = (int64_t)B * N, ps = layout == FLEX_LAYOUT_BCN ? 1 : C, cs = layout == FLEX_LAYOUT_BCN ? N : 1;
     const hipError_t e = with_dtype(dtype, [&](auto t) {
         typedef decltype(t) T;
-        hipLaunchKernelGGL(norm_fwd_kernel<T>, dim3((unsigned)cdiv64(rows, 4)), dim3(256), 0, (hipStream_t)stream, (const T *)x,
-                           weight, bias, (T *)y, mean, rstd, rows, N, C, ps, cs, eps, param_dtype);
-        return hipGetLastError();
+        return launch_norm_fwd<T>((const T *)x, weight, bias, (T *)y, mean, rstd, B, N, C, eps, param_dtype, layout == FLEX_LAYOUT_BCN,
+                                  (hipStream_t)stream);
     });
     return e == hipSuccess ? FLEX_OK : FLEX_ERR_HIP;
 }
@@ -127,7 +692,7 @@ int flexnorm_fwd(const void *x, const void *weight, const void *bias, void *y, f
 size_t flexnorm_bwd_workspace_bytes(int B, int N, int C, int dtype, int layout)
 {
     if (!norm_sizes_ok(B, N, C, layout, dtype, dtype)) return 0;
-    return align256((size_t)norm_slices((int64_t)B * N) * 2 * C * sizeof(float));
+    return align256((size_t)norm_slices(B, N, C, dtype, layout == FLEX_LAYOUT_BCN) * 2 * C * sizeof(float));
 }
 
 int flexnorm_bwd(const void *x, const void *weight, const void *grad_out, const float *mean, const float *rstd, void *grad_x,
@@ -139,21 +704,10 @@ int flexnorm_bwd(const void *x, const void *weight, const void *grad_out, const 
     if (!norm_sizes_ok(B, N, C, layout, dtype, param_dtype) || grad_x == x || grad_x == grad_out) return FLEX_ERR_SHAPE;
     if (grad_weight && (!workspace || ((uintptr_t)workspace & 255) || workspace_bytes < flexnorm_bwd_workspace_bytes(B, N, C, dtype, layout)))
         return FLEX_ERR_WORKSPACE;
-    const int64_t rows = (int64_t)B * N, ps = layout == FLEX_LAYOUT_BCN ? 1 : C, cs = layout == FLEX_LAYOUT_BCN ? N : 1;
-    const hipStream_t s = (hipStream_t)stream;
     const hipError_t e = with_dtype(dtype, [&](auto t) {
         typedef decltype(t) T;
-        if (grad_x)
-            hipLaunchKernelGGL(norm_bwd_kernel<T>, dim3((unsigned)cdiv64(rows, 4)), dim3(256), 0, s, (const T *)x, weight,
-                               (const T *)grad_out, mean, rstd, (T *)grad_x, rows, N, C, ps, cs, param_dtype);
-        if (grad_weight) {
-            const int slices = norm_slices(rows);
-            hipLaunchKernelGGL(norm_params_kernel<T>, dim3((unsigned)((C + 255) / 256), (unsigned)slices), dim3(256), 0, s,
-                               (const T *)x, (const T *)grad_out, mean, rstd, (float *)workspace, rows, cdiv64(rows, slices), N, C, ps, cs);
-            hipLaunchKernelGGL(norm_params_sum_kernel, dim3((unsigned)((C + 255) / 256)), dim3(256), 0, s,
-                               (const float *)workspace, slices, grad_weight, grad_bias, C, param_dtype);
-        }
-        return hipGetLastError();
+        return launch_norm_bwd<T>((const T *)x, weight, (const T *)grad_out, mean, rstd, (T *)grad_x, grad_weight, grad_bias, B, N, C, dtype,
+                                  param_dtype, layout == FLEX_LAYOUT_BCN, (float *)workspace, (hipStream_t)stream);
     });
     return e == hipSuccess ? FLEX_OK : FLEX_ERR_HIP;
 }
