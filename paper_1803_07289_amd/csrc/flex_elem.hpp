@@ -63,21 +63,39 @@ struct Chunk {
     }
 };
 
+// 16 bytes of elements as four words, for what is kept in registers and looked at more than once
+typedef uint32_t Words __attribute__((ext_vector_type(4)));
+template <class T>
+__device__ __forceinline__ void unpack(const Words &w, float (&x)[LANE_ELEMENTS<T>])
+{
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t b = w[i];
+        if constexpr (sizeof(T) == 4) x[i] = __builtin_bit_cast(float, b);
+        else if constexpr (std::is_same<T, bf16>::value) {
+            x[2 * i] = __builtin_bit_cast(float, b << 16);
+            x[2 * i + 1] = __builtin_bit_cast(float, b & 0xFFFF0000u);
+        } else {
+            x[2 * i] = (float)__builtin_bit_cast(_Float16, (uint16_t)b);
+            x[2 * i + 1] = (float)__builtin_bit_cast(_Float16, (uint16_t)(b >> 16));
+        }
+    }
+}
+
 // ---- reductions over groups of L neighbouring lanes, the result on every one of them -----------------------------------------
 // Up to 16 lanes by DPP (quad permutes, then the mirrored half row and row, whose halves hold one value each by then), then by
 // swapping rows of 16 and halves of 32 lanes between a value and its copy; all lanes of a group have to be active.
 
 constexpr int DPP_XOR1 = 0xB1, DPP_XOR2 = 0x4E, DPP_HALF_MIRROR = 0x141, DPP_MIRROR = 0x140;
 
-// op of the two values that swap(v, v) leaves.  They pass through an empty statement: the compiler takes them for one value otherwise
-// where op is a maximum, and leaves that out.
+// op of the two values that swap(v, v) leaves.  (They are taken out of their vector first: a bit cast of a vector's element casts the
+// first one, whichever it is given.)
 template <class V, class Swap, class Op>
 __device__ __forceinline__ V swap_reduce(V v, Swap swap, Op op)
 {
     const unsigned b = __builtin_bit_cast(unsigned, v);
     const auto r = swap(b, b);
-    unsigned one = r[0], two = r[1];
-    asm("" : "+v"(one), "+v"(two));
+    const unsigned one = r[0], two = r[1];
     return op(__builtin_bit_cast(V, one), __builtin_bit_cast(V, two));
 }
 template <int L, class V, class Op>

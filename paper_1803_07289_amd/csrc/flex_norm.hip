@@ -168,16 +168,46 @@ __global__ __launch_bounds__(1024) void norm_long_rows_kernel(const T *__restric
     }
 }
 
-// Backward: a group of L threads walks over rows, its own columns' shares of grad_w and grad_b in registers, which the groups of a
-// workgroup add up in LDS at the end: one partial sum of 2 C a workgroup.
-// PARAMS: with grad_w and grad_b (gx may be null then); otherwise only gx.
-template <class T, int L, int U, bool PARAMS, bool NARROW>
-__global__ __launch_bounds__(L > 256 ? L : 256) void norm_rows_bwd_kernel(const T *__restrict__ x, Param<T> w, const T *__restrict__ g,
-                                                                          const float *__restrict__ mean, const float *__restrict__ rstd,
-                                                                          T *__restrict__ gx, float *__restrict__ partials,
-                                                                          int64_t rows, int C)
+// Two sums at once, over the L threads of each row of a workgroup.
+template <int L, int WAVES>
+__device__ __forceinline__ void row_sums(float &a, float &b, float (*place)[WAVES])
 {
-    constexpr int N = LANE_ELEMENTS<T>, WG = L > 256 ? L : 256, G = WG / L;
+    if (L <= 64) {
+        a = lanes_sum<L <= 64 ? L : 64>(a);
+        b = lanes_sum<L <= 64 ? L : 64>(b);
+        return;
+    }
+    a = lanes_sum<64>(a);
+    b = lanes_sum<64>(b);
+    const int wave = threadIdx.x >> 6, first = wave / (L / 64) * (L / 64);
+    if ((threadIdx.x & 63) == 0) {
+        place[0][wave] = a;
+        place[1][wave] = b;
+    }
+    __syncthreads();
+    a = place[0][first];
+    b = place[1][first];
+#pragma unroll
+    for (int i = 1; i < L / 64; ++i) {
+        a += place[0][first + i];
+        b += place[1][first + i];
+    }
+}
+
+// Backward: groups of L threads walk over rows, the next row of each on its way, their columns' shares of grad_w and grad_b in
+// registers; those of a workgroup's groups are added up at the end: one partial sum of 2 C a workgroup, and one workgroup of two
+// groups to a compute unit where rows take 256 threads (8188 x 5120 bf16: 256 partial sums are 10 MB, of the 252 that have to move).
+// A row stays as it was read until its gradient is written: twice the conversions, half the registers.
+// PARAMS: with grad_w and grad_b (gx may be null then); otherwise only gx.
+constexpr int rows_bwd_threads(int L) { return L == 256 ? 512 : L > 256 ? L : 256; }
+template <class T, int L, int U, bool PARAMS, bool NARROW>
+__global__ __launch_bounds__(rows_bwd_threads(L)) void norm_rows_bwd_kernel(const T *__restrict__ x, Param<T> w, const T *__restrict__ g,
+                                                                            const float *__restrict__ mean, const float *__restrict__ rstd,
+                                                                            T *__restrict__ gx, float *__restrict__ partials,
+                                                                            int64_t rows, int C)
+{
+    constexpr int N = LANE_ELEMENTS<T>, WG = rows_bwd_threads(L), G = WG / L;
+    typedef typename Chunk<T>::V V;
     __shared__ float s_place[2][2][WG / 64];
     const int sub = threadIdx.x % L, group = threadIdx.x / L;
     const float count = (float)C;
@@ -199,54 +229,84 @@ __global__ __launch_bounds__(L > 256 ? L : 256) void norm_rows_bwd_kernel(const 
         }
     }
     const int64_t step = (int64_t)gridDim.x * G;
-    int turn = 0;
-    // (a workgroup's groups take as many turns as each other: lanes and barriers stay together)
-    for (int64_t first = (int64_t)blockIdx.x * G; first < rows; first += step, turn ^= 1) {
+    Words xn[U], gn[U];
+    float mn, rn;
+    auto request = [&](int64_t first) {
         const int64_t row = min(first + group, rows - 1);
-        const bool mine = first + group < rows;
-        float xh[U][N], gg[U][N];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int c0 = (u * L + sub) * N;
             if (NARROW) {
+                V a, b;
 #pragma unroll
                 for (int j = 0; j < N; ++j) {
-                    xh[u][j] = c0 + j < C ? to_f32(x[row * C + c0 + j]) : 0.f;
-                    gg[u][j] = c0 + j < C ? to_f32(g[row * C + c0 + j]) : 0.f;
+                    a[j] = c0 + j < C ? x[row * C + c0 + j] : (T)0.f;
+                    b[j] = c0 + j < C ? g[row * C + c0 + j] : (T)0.f;
                 }
+                xn[u] = __builtin_bit_cast(Words, a);
+                gn[u] = __builtin_bit_cast(Words, b);
             } else {
-                Chunk<T>::load(x + row * C + Chunk<T>::from(c0, C), xh[u]);
-                Chunk<T>::load(g + row * C + Chunk<T>::from(c0, C), gg[u]);
+                xn[u] = __builtin_bit_cast(Words, *(const V *)(x + row * C + Chunk<T>::from(c0, C)));
+                gn[u] = __builtin_bit_cast(Words, *(const V *)(g + row * C + Chunk<T>::from(c0, C)));
             }
         }
-        const float m = mean[row], r = rstd[row];
+        mn = mean[row];
+        rn = rstd[row];
+    };
+    request((int64_t)blockIdx.x * G);
+    int turn = 0;
+    // (a workgroup's groups take as many turns as each other: lanes and barriers stay together)
+    for (int64_t first = (int64_t)blockIdx.x * G; first < rows; first += step, turn ^= 1) {
+        const int64_t row = first + group;
+        const bool mine = row < rows;
+        Words xr[U], gr[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            xr[u] = xn[u];
+            gr[u] = gn[u];
+        }
+        const float m = mn, r = rn;
+        if (first + step < rows) request(first + step);
         float s1 = 0.f, s2 = 0.f;
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            if (!NARROW) Chunk<T>::mask(gg[u], (u * L + sub) * N, C, 0.f);
+            const int c0 = (u * L + sub) * N;
+            float xx[N], gg[N];
+            unpack<T>(xr[u], xx);
+            unpack<T>(gr[u], gg);
+            if (!mine || (!NARROW && c0 + N > C))       // rows behind the last, columns that are another lane's: no gradient
+#pragma unroll
+                for (int j = 0; j < N; ++j)
+                    if (!mine || C - N + j < c0) gg[j] = 0.f;
 #pragma unroll
             for (int j = 0; j < N; ++j) {
-                xh[u][j] = (xh[u][j] - m) * r;
-                const float h = gg[u][j] * ww[u][j];
+                const float xh = (xx[j] - m) * r, h = gg[j] * ww[u][j];
                 s1 += h;
-                s2 += h * xh[u][j];
-                if (PARAMS && mine) {
-                    gw[u][j] += gg[u][j] * xh[u][j];
-                    gb[u][j] += gg[u][j];
+                s2 += h * xh;
+                if (PARAMS) {
+                    gw[u][j] += gg[j] * xh;
+                    gb[u][j] += gg[j];
                 }
             }
         }
         if (PARAMS && !gx) continue;
-        s1 = row_sum<L>(s1, s_place[turn][0]) / count;
-        s2 = row_sum<L>(s2, s_place[turn][1]) / count;
+        row_sums<L>(s1, s2, s_place[turn]);
+        s1 /= count;
+        s2 /= count;
         if (!mine) continue;
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int c0 = (u * L + sub) * N;
             if (c0 >= C) break;
-            float out[N];
+            if (sizeof(T) == 2) asm("" : "+v"(xr[u]), "+v"(gr[u]));       // converted again here, and not kept from above
+            float xx[N], gg[N], out[N];
+            unpack<T>(xr[u], xx);
+            unpack<T>(gr[u], gg);
 #pragma unroll
-            for (int j = 0; j < N; ++j) out[j] = (gg[u][j] * ww[u][j] - s1 - xh[u][j] * s2) * r;
+            for (int j = 0; j < N; ++j) {
+                const float xh = (xx[j] - m) * r, h = gg[j] * ww[u][j];
+                out[j] = (h - s1 - xh * s2) * r;
+            }
             T *to = gx + row * C;
             if (c0 + N <= C) Chunk<T>::store(to + c0, out);
             else {
@@ -258,33 +318,38 @@ __global__ __launch_bounds__(L > 256 ? L : 256) void norm_rows_bwd_kernel(const 
         }
     }
     if (!PARAMS) return;
-    // (each group's columns begin at c0; what a clamped lane holds before that is zero, its gradient having been masked)
-    __shared__ float s_sum[L < 256 ? 2 * 256 * U * N : 1];
+    // groups of one wave by lane, then those of the workgroup (waves, or groups of several) through LDS
+    constexpr int LL = L < 64 ? 64 : L, GG = WG / LL;
+    __shared__ float s_sum[GG > 1 ? (GG - 1) * L * U * N : 1];
+    const int other = threadIdx.x / LL;
     float *const to = partials + (int64_t)blockIdx.x * 2 * C;
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-        const int c0 = (u * L + sub) * N, from = NARROW ? c0 : Chunk<T>::from(c0, C);
+    for (int which = 0; which < 2; ++which) {
+        float (&acc)[U][N] = which ? gb : gw;
 #pragma unroll
-        for (int j = 0; j < N; ++j) {
-            if (L < 256) {
-                s_sum[((group * U + u) * N + j) * L + sub] = gw[u][j];
-                s_sum[((group * U + u) * N + j) * L + sub + 256 * U * N] = gb[u][j];
-            } else if (from + j >= c0 && from + j < C) {
-                to[from + j] = gw[u][j];
-                to[C + from + j] = gb[u][j];
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int j = 0; j < N; ++j) {
+                for (int o = L; o < 64; o <<= 1) acc[u][j] += __shfl_xor(acc[u][j], o);
+                if (other > 0 && threadIdx.x % LL < L) s_sum[((other - 1) * U * N + u * N + j) * L + sub] = acc[u][j];
+            }
+        if (GG > 1) __syncthreads();
+        if (threadIdx.x < L) {
+#pragma unroll 1
+            for (int k = 0; k < GG - 1; ++k)
+#pragma unroll
+                for (int u = 0; u < U; ++u)
+#pragma unroll
+                    for (int j = 0; j < N; ++j) acc[u][j] += s_sum[(k * U * N + u * N + j) * L + sub];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int c0 = (u * L + sub) * N, from = NARROW ? c0 : Chunk<T>::from(c0, C);
+#pragma unroll
+                for (int j = 0; j < N; ++j)
+                    if (from + j >= c0 && from + j < C) to[which * C + from + j] = acc[u][j];
             }
         }
-    }
-    if (L >= 256) return;
-    __syncthreads();
-    for (int i = threadIdx.x; i < 2 * L * U * N; i += 256) {
-        const int which = i / (L * U * N), at = i % (L * U * N);
-        float sum = 0.f;
-#pragma unroll
-        for (int k = 0; k < G; ++k) sum += s_sum[which * 256 * U * N + k * (U * N * L) + at];
-        const int lane = at % L, j = at / L % N, u = at / L / N;
-        const int c0 = (u * L + lane) * N, from = NARROW ? c0 : Chunk<T>::from(c0, C);
-        if (from + j >= c0 && from + j < C) to[which * C + from + j] = sum;
+        if (GG > 1) __syncthreads();
     }
 }
 
@@ -552,6 +617,7 @@ static bool with_row_threads(int C, F f)
     FLEX_ROW_THREADS(64, 2)
     FLEX_ROW_THREADS(256, 1)
     FLEX_ROW_THREADS(256, 2)
+    FLEX_ROW_THREADS(256, 3)
     FLEX_ROW_THREADS(256, 4)
     FLEX_ROW_THREADS(1024, 2)
     if constexpr (N == 4) FLEX_ROW_THREADS(1024, 4)
@@ -572,7 +638,7 @@ static void with_col_waves(int C, F f)
     else f(std::integral_constant<int, 16>{});
 }
 
-// Partial sums of grad_w and grad_b: the workgroups that walk over the positions, at least four turns to each.
+// Partial sums of grad_w and grad_b: the workgroups that walk over the positions, four turns at least to each.
 static int norm_slices(int B, int N, int C, int dtype, bool bcn)
 {
     const int64_t rows = (int64_t)B * N, cus = device_cu_count();
@@ -583,9 +649,10 @@ static int norm_slices(int B, int N, int C, int dtype, bool bcn)
     }
     if (C > ROW_CHANNELS_MAX) return (int)std::min<int64_t>(64, cdiv64(rows, 16));
     const int lane = 16 / (int)dtype_bytes(dtype);
-    int64_t groups = 1;
-    for (const int L : {4, 8, 16, 32, 64}) if (C <= L * lane || (L == 64 && C <= 128 * lane)) { groups = 256 / L; break; }
-    return (int)std::max<int64_t>(1, std::min<int64_t>(cdiv64(rows, 4 * groups), groups > 1 ? 4 * cus : 2 * cus));
+    int groups = C <= 256 * 4 * lane ? 2 : 1;
+    for (const int L : {64, 32, 16, 8, 4})
+        if (C <= (L == 64 ? 128 : L) * lane) groups = 256 / L;
+    return (int)std::max<int64_t>(1, std::min<int64_t>(cdiv64(rows, 4 * groups), groups > 2 ? 4 * cus : cus));
 }
 
 template <class T>
@@ -640,7 +707,7 @@ static hipError_t launch_norm_bwd(const T *x, const void *weight, const T *g, co
                                partials, rows, cdiv64(rows, slices), N, C);
     } else if (!with_row_threads<T>(C, [&](auto l, auto u) {
                    constexpr int L = decltype(l)::value, U = decltype(u)::value;
-                   const dim3 wg(std::max(L, 256)), grid((unsigned)(gw ? slices : cdiv64(rows, std::max(256 / L, 1))));
+                   const dim3 wg(rows_bwd_threads(L)), grid((unsigned)(gw ? slices : cdiv64(rows, rows_bwd_threads(L) / L)));
                    auto launch = [&](auto params, auto narrow) {
                        hipLaunchKernelGGL((norm_rows_bwd_kernel<T, L, U, decltype(params)::value, decltype(narrow)::value>), grid, wg, 0, s, x,
                                           w, g, mean, rstd, gx, partials, rows, C);
