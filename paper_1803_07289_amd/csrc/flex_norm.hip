@@ -70,9 +70,12 @@ __global__ __launch_bounds__(L > 256 ? L : 256) void norm_rows_kernel(const T *_
         float sum = 0.f;
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            if (!NARROW) Chunk<T>::mask(v[r][u], (u * L + sub) * N, C, 0.f);
+            float own[N];
 #pragma unroll
-            for (int j = 0; j < N; ++j) sum += v[r][u][j];
+            for (int j = 0; j < N; ++j) own[j] = v[r][u][j];
+            if (!NARROW) Chunk<T>::mask(own, (u * L + sub) * N, C, 0.f);
+#pragma unroll
+            for (int j = 0; j < N; ++j) sum += own[j];
         }
         mean[r] = row_sum<L>(sum, s_place[2 * r]) / count;
     }
@@ -123,12 +126,13 @@ __global__ __launch_bounds__(L > 256 ? L : 256) void norm_rows_kernel(const T *_
                 out[j] = (v[r][u][j] - mean[r]) * rstd[r];
                 if (w.p) out[j] = out[j] * ww[j] + bb[j];
             }
-            T *to = y + row * C + c0;
-            if (c0 + N <= C) Chunk<T>::store(to, out);
-            else
+            T *to = y + row * C;
+            if (NARROW) {
 #pragma unroll
                 for (int j = 0; j < N; ++j)
-                    if (from + j >= c0 && from + j < C) y[row * C + from + j] = (T)out[j];
+                    if (c0 + j < C) to[c0 + j] = (T)out[j];
+            } else
+                Chunk<T>::store(to + from, out);        // (columns of another lane's too: the same values)
         }
     }
     if (sub == 0)
@@ -195,44 +199,41 @@ __device__ __forceinline__ void row_sums(float &a, float &b, float (*place)[WAVE
 }
 
 // Backward: groups of L threads walk over rows, the next row of each on its way, their columns' shares of grad_w and grad_b in
-// registers; those of a workgroup's groups are added up at the end: one partial sum of 2 C a workgroup, and one workgroup of two
-// groups to a compute unit where rows take 256 threads (8188 x 5120 bf16: 256 partial sums are 10 MB, of the 252 that have to move).
-// A row stays as it was read until its gradient is written: twice the conversions, half the registers.
+// registers; those of a workgroup's groups are added up at the end: one partial sum of 2 C a workgroup, and one workgroup to a
+// compute unit where rows take 256 threads or more (8188 x 5120 bf16: 256 partial sums are 10 MB, of the 252 that have to move).
+// A row stays as it was read and is converted twice, for its two sums and for its results: half the registers.  The weights are in
+// LDS where rows are long: read from memory they would queue behind the next row.  No store is in a branch: a wait for the next
+// row could not be told from one for the store then.  Lanes past a row's end and groups past the last row store what another one
+// stores too, the same values.
 // PARAMS: with grad_w and grad_b (gx may be null then); otherwise only gx.
-constexpr int rows_bwd_threads(int L) { return L == 256 ? 512 : L > 256 ? L : 256; }
+// Threads of a workgroup: as many as find their registers (two sums and two rows' 16 bytes for each piece of U, and some 60 more).
+constexpr int rows_bwd_threads(int L, int U, int N) { return L < 256 ? 256 : L > 256 || U * N <= 16 ? 1024 : 512; }
 template <class T, int L, int U, bool PARAMS, bool NARROW>
-__global__ __launch_bounds__(rows_bwd_threads(L)) void norm_rows_bwd_kernel(const T *__restrict__ x, Param<T> w, const T *__restrict__ g,
+__global__ __launch_bounds__(rows_bwd_threads(L, U, LANE_ELEMENTS<T>)) void norm_rows_bwd_kernel(const T *__restrict__ x, Param<T> w, const T *__restrict__ g,
                                                                             const float *__restrict__ mean, const float *__restrict__ rstd,
                                                                             T *__restrict__ gx, float *__restrict__ partials,
                                                                             int64_t rows, int C)
 {
-    constexpr int N = LANE_ELEMENTS<T>, WG = rows_bwd_threads(L), G = WG / L;
+    constexpr int N = LANE_ELEMENTS<T>, WG = rows_bwd_threads(L, U, N), G = WG / L;
+    constexpr bool SHARED = L >= 256;
     typedef typename Chunk<T>::V V;
     __shared__ float s_place[2][2][WG / 64];
+    __shared__ __attribute__((aligned(16))) float s_weight[SHARED ? L * U * N : 1];
     const int sub = threadIdx.x % L, group = threadIdx.x / L;
     const float count = (float)C;
-    float ww[U][N], gw[U][N], gb[U][N];
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-        const int c0 = (u * L + sub) * N;
-#pragma unroll
-        for (int j = 0; j < N; ++j) {
-            ww[u][j] = 1.f;
-            gw[u][j] = gb[u][j] = 0.f;
-        }
-        if (w.p) {
-            if (NARROW) {
-#pragma unroll
-                for (int j = 0; j < N; ++j) ww[u][j] = c0 + j < C ? w[c0 + j] : 0.f;
-            } else
-                w.load(Chunk<T>::from(c0, C), ww[u]);
-        }
-    }
     const int64_t step = (int64_t)gridDim.x * G;
-    Words xn[U], gn[U];
-    float mn, rn;
-    auto request = [&](int64_t first) {
+    struct Row {
+        Words x[U], g[U];
+        float mean, rstd;
+    } one, two;
+    // (one row to a wave: its address in scalar registers)
+    auto row_of = [&](int64_t first) {
         const int64_t row = min(first + group, rows - 1);
+        return L < 64 ? row : (int64_t)__builtin_amdgcn_readfirstlane((int)row);
+    };
+    auto request = [&](Row &to, int64_t first) {
+        const int64_t row = row_of(first);
+        const T *const xrow = x + row * C, *const grow = g + row * C;
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int c0 = (u * L + sub) * N;
@@ -240,82 +241,127 @@ __global__ __launch_bounds__(rows_bwd_threads(L)) void norm_rows_bwd_kernel(cons
                 V a, b;
 #pragma unroll
                 for (int j = 0; j < N; ++j) {
-                    a[j] = c0 + j < C ? x[row * C + c0 + j] : (T)0.f;
-                    b[j] = c0 + j < C ? g[row * C + c0 + j] : (T)0.f;
+                    a[j] = c0 + j < C ? xrow[c0 + j] : (T)0.f;
+                    b[j] = c0 + j < C ? grow[c0 + j] : (T)0.f;
                 }
-                xn[u] = __builtin_bit_cast(Words, a);
-                gn[u] = __builtin_bit_cast(Words, b);
+                to.x[u] = __builtin_bit_cast(Words, a);
+                to.g[u] = __builtin_bit_cast(Words, b);
             } else {
-                xn[u] = __builtin_bit_cast(Words, *(const V *)(x + row * C + Chunk<T>::from(c0, C)));
-                gn[u] = __builtin_bit_cast(Words, *(const V *)(g + row * C + Chunk<T>::from(c0, C)));
+                to.x[u] = __builtin_bit_cast(Words, *(const V *)(xrow + (unsigned)Chunk<T>::from(c0, C)));
+                to.g[u] = __builtin_bit_cast(Words, *(const V *)(grow + (unsigned)Chunk<T>::from(c0, C)));
             }
         }
-        mn = mean[row];
-        rn = rstd[row];
+        to.mean = mean[row];
+        to.rstd = rstd[row];
     };
-    request((int64_t)blockIdx.x * G);
-    int turn = 0;
-    // (a workgroup's groups take as many turns as each other: lanes and barriers stay together)
-    for (int64_t first = (int64_t)blockIdx.x * G; first < rows; first += step, turn ^= 1) {
-        const int64_t row = first + group;
-        const bool mine = row < rows;
-        Words xr[U], gr[U];
+    int64_t first = (int64_t)blockIdx.x * G;
+    request(one, first);
+    float own_w[SHARED ? 1 : U][N], gw[U][N], gb[U][N];
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            xr[u] = xn[u];
-            gr[u] = gn[u];
+    for (int u = 0; u < U; ++u) {
+        const int c0 = (u * L + sub) * N;
+        float ww[N];
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+            ww[j] = 1.f;
+            gw[u][j] = gb[u][j] = 0.f;
         }
-        const float m = mn, r = rn;
-        if (first + step < rows) request(first + step);
+        if (w.p && (!SHARED || group == 0)) {
+            if (NARROW) {
+#pragma unroll
+                for (int j = 0; j < N; ++j) ww[j] = c0 + j < C ? w[c0 + j] : 0.f;
+            } else
+                w.load(Chunk<T>::from(c0, C), ww);
+        }
+        if (SHARED && group == 0) Chunk<float, N>::store(s_weight + c0, ww);
+        if (!SHARED)
+#pragma unroll
+            for (int j = 0; j < N; ++j) own_w[SHARED ? 0 : u][j] = ww[j];
+    }
+    if (SHARED) __syncthreads();
+    auto weights = [&](int u, float (&ww)[N]) {
+        if (SHARED) {
+#pragma unroll
+            for (int j = 0; j < N; j += 4) {
+                const v4f four = *(const v4f *)(s_weight + (u * L + sub) * N + j);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) ww[j + k] = four[k];
+            }
+        } else
+#pragma unroll
+            for (int j = 0; j < N; ++j) ww[j] = own_w[SHARED ? 0 : u][j];
+    };
+    int turn = 0;
+    auto take = [&](Row &now, Row &then, int64_t first) {
+        const bool mine = first + group < rows;
+        T *const to = gx + row_of(first) * C;
+        request(then, first + step);        // (behind the last row: the last one again)
+        Words (&xr)[U] = now.x, (&gr)[U] = now.g;
+        const float m = now.mean, r = now.rstd;
         float s1 = 0.f, s2 = 0.f;
+        if (!PARAMS || gx) {
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int skip = NARROW ? 0 : (u * L + sub) * N + N - C;       // columns that are another lane's
+                float xx[N], gg[N], ww[N];
+                unpack<T>(xr[u], xx);
+                unpack<T>(gr[u], gg);
+                weights(u, ww);
+                if (skip > 0)
+#pragma unroll
+                    for (int j = 0; j < N; ++j) gg[j] = j < skip ? 0.f : gg[j];
+#pragma unroll
+                for (int j = 0; j < N; ++j) {
+                    const float xh = (xx[j] - m) * r, h = gg[j] * ww[j];
+                    s1 += h;
+                    s2 += h * xh;
+                }
+                if (U > 1) __builtin_amdgcn_sched_barrier(0);       // (the pieces one after the other, in the same registers)
+            }
+            row_sums<L>(s1, s2, s_place[turn]);
+            s1 /= count;
+            s2 /= count;
+        }
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const int c0 = (u * L + sub) * N;
+            const int c0 = (u * L + sub) * N, skip = !mine ? N : NARROW ? 0 : c0 + N - C;
+            if (sizeof(T) == 2) asm("" : "+v"(xr[u]), "+v"(gr[u]));       // converted again here, and not kept from above
             float xx[N], gg[N];
             unpack<T>(xr[u], xx);
             unpack<T>(gr[u], gg);
-            if (!mine || (!NARROW && c0 + N > C))       // rows behind the last, columns that are another lane's: no gradient
 #pragma unroll
-                for (int j = 0; j < N; ++j)
-                    if (!mine || C - N + j < c0) gg[j] = 0.f;
+            for (int j = 0; j < N; ++j) xx[j] = (xx[j] - m) * r;
+            if (!PARAMS || gx) {
+                float ww[N], out[N];
+                weights(u, ww);
+#pragma unroll
+                for (int j = 0; j < N; ++j) out[j] = (gg[j] * ww[j] - s1 - xx[j] * s2) * r;
+                if (NARROW) {
+#pragma unroll
+                    for (int j = 0; j < N; ++j)
+                        if (c0 + j < C) to[c0 + j] = (T)out[j];
+                } else
+                    Chunk<T>::store(to + (unsigned)Chunk<T>::from(c0, C), out);
+            }
+            if (!PARAMS) continue;
+            if (skip > 0)
+#pragma unroll
+                for (int j = 0; j < N; ++j) gg[j] = j < skip ? 0.f : gg[j];
 #pragma unroll
             for (int j = 0; j < N; ++j) {
-                const float xh = (xx[j] - m) * r, h = gg[j] * ww[u][j];
-                s1 += h;
-                s2 += h * xh;
-                if (PARAMS) {
-                    gw[u][j] += gg[j] * xh;
-                    gb[u][j] += gg[j];
-                }
+                gw[u][j] += gg[j] * xx[j];
+                gb[u][j] += gg[j];
             }
+            if (U > 1) __builtin_amdgcn_sched_barrier(0);
         }
-        if (PARAMS && !gx) continue;
-        row_sums<L>(s1, s2, s_place[turn]);
-        s1 /= count;
-        s2 /= count;
-        if (!mine) continue;
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int c0 = (u * L + sub) * N;
-            if (c0 >= C) break;
-            if (sizeof(T) == 2) asm("" : "+v"(xr[u]), "+v"(gr[u]));       // converted again here, and not kept from above
-            float xx[N], gg[N], out[N];
-            unpack<T>(xr[u], xx);
-            unpack<T>(gr[u], gg);
-#pragma unroll
-            for (int j = 0; j < N; ++j) {
-                const float xh = (xx[j] - m) * r, h = gg[j] * ww[u][j];
-                out[j] = (h - s1 - xh * s2) * r;
-            }
-            T *to = gx + row * C;
-            if (c0 + N <= C) Chunk<T>::store(to + c0, out);
-            else {
-                const int from = NARROW ? c0 : Chunk<T>::from(c0, C);
-#pragma unroll
-                for (int j = 0; j < N; ++j)
-                    if (from + j >= c0 && from + j < C) to[from + j] = (T)out[j];
-            }
-        }
+        turn ^= 1;
+    };
+    // (a workgroup's groups take as many turns as each other: lanes and barriers stay together)
+    while (true) {
+        take(one, two, first);
+        if ((first += step) >= rows) break;
+        take(two, one, first);
+        if ((first += step) >= rows) break;
     }
     if (!PARAMS) return;
     // groups of one wave by lane, then those of the workgroup (waves, or groups of several) through LDS
@@ -412,6 +458,12 @@ __device__ __forceinline__ float waves_sum(float v, float (*place)[64])
     return v;
 }
 
+// what lane i has, on all of them (a channel's weight: one load for R of them)
+__device__ __forceinline__ float lane_value(float v, int i)
+{
+    return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), i));
+}
+
 template <class T, int W, int R>
 __global__ __launch_bounds__(64 * W) void norm_cols_kernel(const T *__restrict__ x, Param<T> w, Param<T> b, T *__restrict__ y,
                                                            float *mean_out, float *rstd_out, int N, int C, float eps)
@@ -433,6 +485,7 @@ __global__ __launch_bounds__(64 * W) void norm_cols_kernel(const T *__restrict__
         for (int i = 0; i < R; ++i) sum += v[i];
     } else
         for (int c = first; c < last; ++c) sum += to_f32(x[base + (int64_t)c * N]);
+    const float ww = R && w.p && lane < last - first ? w[first + lane] : 1.f, bb = R && w.p && lane < last - first ? b[first + lane] : 0.f;
     const float mean = waves_sum<W>(sum, s_place[0]) / count;
     if (R) {
 #pragma unroll
@@ -446,17 +499,20 @@ __global__ __launch_bounds__(64 * W) void norm_cols_kernel(const T *__restrict__
             sq += d * d;
         }
     const float rstd = 1.f / sqrtf(waves_sum<W>(sq, s_place[1]) / count + eps);
-    if (!mine) return;
-    auto put = [&](int c, float value) {
-        const float d = (value - mean) * rstd;
-        y[base + (int64_t)c * N] = (T)(w.p ? d * w[c] + b[c] : d);
-    };
     if (R) {
 #pragma unroll
+        for (int i = 0; i < R; ++i) v[i] = (v[i] - mean) * rstd * lane_value(ww, i) + lane_value(bb, i);
+        if (!mine) return;
+#pragma unroll
         for (int i = 0; i < R; ++i)
-            if (first + i < last) put(first + i, v[i]);
-    } else
-        for (int c = first; c < last; ++c) put(c, to_f32(x[base + (int64_t)c * N]));
+            if (first + i < last) y[base + (int64_t)(first + i) * N] = (T)v[i];
+    } else {
+        if (!mine) return;
+        for (int c = first; c < last; ++c) {
+            const float d = (to_f32(x[base + (int64_t)c * N]) - mean) * rstd;
+            y[base + (int64_t)c * N] = (T)(w.p ? d * w[c] + b[c] : d);
+        }
+    }
     if (wave == 0) {
         if (mean_out) mean_out[cloud * N + n] = mean;
         if (rstd_out) rstd_out[cloud * N + n] = rstd;
@@ -476,6 +532,7 @@ __global__ __launch_bounds__(64 * W) void norm_cols_bwd_kernel(const T *__restri
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int first = wave * R, many = min(R, C - first);
     const float count = (float)C;
+    const float ww = w.p && lane < many ? w[first + lane] : 1.f;
     float gw[R], gb[R];
 #pragma unroll
     for (int i = 0; i < R; ++i) gw[i] = gb[i] = 0.f;
@@ -495,7 +552,7 @@ __global__ __launch_bounds__(64 * W) void norm_cols_bwd_kernel(const T *__restri
 #pragma unroll
         for (int i = 0; i < R; ++i) {
             xh[i] = (xh[i] - m) * r;
-            const float h = i < many && w.p ? gg[i] * w[first + i] : gg[i];
+            const float h = gg[i] * lane_value(ww, i);
             s1 += h;
             s2 += h * xh[i];
             if (PARAMS) {
@@ -506,13 +563,11 @@ __global__ __launch_bounds__(64 * W) void norm_cols_bwd_kernel(const T *__restri
         if (PARAMS && !gx) continue;
         s1 = waves_sum<W>(s1, s_place[turn][0]) / count;
         s2 = waves_sum<W>(s2, s_place[turn][1]) / count;
-        if (!mine) continue;
 #pragma unroll
-        for (int i = 0; i < R; ++i)
-            if (i < many) {
-                const float h = w.p ? gg[i] * w[first + i] : gg[i];
-                gx[base + (int64_t)i * N] = (T)((h - s1 - xh[i] * s2) * r);
-            }
+        for (int i = 0; i < R; ++i) {
+            const float out = (gg[i] * lane_value(ww, i) - s1 - xh[i] * s2) * r;
+            if (i < many && mine) gx[base + (int64_t)i * N] = (T)out;
+        }
     }
     if (!PARAMS) return;
 #pragma unroll
@@ -652,7 +707,7 @@ static int norm_slices(int B, int N, int C, int dtype, bool bcn)
     int groups = C <= 256 * 4 * lane ? 2 : 1;
     for (const int L : {64, 32, 16, 8, 4})
         if (C <= (L == 64 ? 128 : L) * lane) groups = 256 / L;
-    return (int)std::max<int64_t>(1, std::min<int64_t>(cdiv64(rows, 4 * groups), groups > 2 ? 4 * cus : cus));
+    return (int)std::max<int64_t>(1, std::min<int64_t>(cdiv64(rows, 4 * groups), C <= 128 * lane ? 4 * cus : cus));
 }
 
 template <class T>
@@ -707,7 +762,8 @@ static hipError_t launch_norm_bwd(const T *x, const void *weight, const T *g, co
                                partials, rows, cdiv64(rows, slices), N, C);
     } else if (!with_row_threads<T>(C, [&](auto l, auto u) {
                    constexpr int L = decltype(l)::value, U = decltype(u)::value;
-                   const dim3 wg(rows_bwd_threads(L)), grid((unsigned)(gw ? slices : cdiv64(rows, rows_bwd_threads(L) / L)));
+                   constexpr int WG = rows_bwd_threads(L, U, LANE_ELEMENTS<T>);
+                   const dim3 wg(WG), grid((unsigned)(gw ? slices : cdiv64(rows, WG / L)));
                    auto launch = [&](auto params, auto narrow) {
                        hipLaunchKernelGGL((norm_rows_bwd_kernel<T, L, U, decltype(params)::value, decltype(narrow)::value>), grid, wg, 0, s, x,
                                           w, g, mean, rstd, gx, partials, rows, C);
