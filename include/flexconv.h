@@ -478,7 +478,7 @@ int flexlogp_bwd(const void *logits, const int32_t *target, const float *lse, co
  * flexadamw_plan_build enters the tensors in device memory of the caller (plan: flexadamw_plan_bytes, 256-byte aligned), which also
  * holds the step's number, so that a captured step counts on in every replay; it fills *out, a handle of plain values for
  * flexadamw_step.  The plan is valid as long as the tensors stay where they are; calls that share one must be stream-ordered.
- * `steps`: how many steps were done before (0 for a new run; the int64 at FLEX_ADAMW_STEPS_AT bytes of the plan is the count).
+ * 0 <= beta1, beta2 < 1; eps a normal fp32 number.  `steps`: how many steps were done before (0 for a new run; the int64 at FLEX_ADAMW_STEPS_AT bytes of the plan is the count).
  *   tensors   host array of n (n <= 2^20); count < 2^31 elements, 0 allowed; no memory twice in the list
  *   state_bits 32: exp_avg, exp_avg_sq fp32 [count].  8: e4m3 (OCP) bytes [count] and a power of two (e8m0 byte) for every 32 of
  *             them, [ceil(count / 32)]; exp_avg_sq holds roots: v = (value * scale)^2.  A state is rounded up or down at random so

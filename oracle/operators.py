@@ -132,7 +132,7 @@ def store(x, r, root=None):
     ey = np.maximum(_exponent(y), -6)
     f = _power(3 - ey)
     if root is None:
-        steps = np.floor(y * f + r)
+        steps = np.floor((y * f).astype(np.float64) + r)      # (the sum not rounded)
     else:
         steps = np.floor(y * f)
         f = f * _power(-e)[:, None]

@@ -6,8 +6,8 @@
 // never move it: states are rounded at random, with probabilities that make the mean exact.  v is kept by its root, which spreads
 // its range over twice the exponents; the choice between two roots is made so that the square has the right mean, and a v
 // above zero is never stored as zero, which would leave eps alone under m.  The random bits are a hash of (seed, step,
-// tensor, element).  Every operation here is rounded by itself (no fused multiply-adds), so that states are the same bits
-// wherever the formulas are evaluated in fp32.
+// tensor, element).  What leads to a state is rounded operation by operation (no fused multiply-adds but where they are exact), so
+// that states are the same bits wherever the formulas are evaluated in fp32.
 #include "flex_elem.hpp"
 #include <algorithm>
 #include <math.h>
@@ -108,16 +108,14 @@ __global__ __launch_bounds__(ADAMW_GRADS) void adamw_begin_kernel(AdamwPlan plan
 // ---- states in 8 bits --------------------------------------------------------------------------------------------------
 
 __device__ __forceinline__ float power2(int e) { return __builtin_bit_cast(float, (uint32_t)(e + 127) << 23); }
-__device__ __forceinline__ int exponent2(float x) { return (int)(__builtin_bit_cast(uint32_t, x) >> 23 & 0xFF) - 127; }
 
 // The largest of a block's magnitudes: 8 to a lane, four lanes.
 __device__ __forceinline__ float block_max(const float (&x)[8])
 {
-    float m = x[0];
+    float m = fabsf(x[0]);
 #pragma unroll
-    for (int i = 1; i < 8; ++i) m = fmaxf(m, x[i]);
-    m = fmaxf(m, __shfl_xor(m, 1));
-    return fmaxf(m, __shfl_xor(m, 2));
+    for (int i = 1; i < 8; ++i) m = fmaxf(m, fabsf(x[i]));
+    return lanes_max<4>(m);
 }
 
 // The exponent that brings `largest` to (224, 448]; within [-100, 120], so that the powers below stay in fp32.
@@ -128,17 +126,34 @@ __device__ __forceinline__ int block_exponent(float largest)
     return min(max(e, -100), 120);
 }
 
-__device__ __forceinline__ void store_codes(uint8_t *codes, uint8_t *scale, const uint32_t (&code)[8], int e, int64_t at, int64_t count)
+// The state that lies up or down from `value` (a first moment times its block's scale) by 16 random bits in the upper half of r: the
+// hardware's conversion, which adds them below the last bit kept, subnormals too.  Into byte i of word.
+template <int i>
+__device__ __forceinline__ uint32_t first_code(float value, uint32_t r, uint32_t word)
+{
+    return (uint32_t)__builtin_amdgcn_cvt_sr_fp8_f32(value, (int)r, (int)word, i);
+}
+// The state of a second moment v, its root and the scale of its block: in steps of e4m3 at the root's exponent, n below it and n + 1 above
+// it, their squares n^2 and n^2 + 2 n + 1; up where the random share of the difference lies below v.
+__device__ __forceinline__ uint32_t second_code(float v, float root, float down, uint32_t r16)
+{
+    const float y = root * down;
+    const uint32_t bits = __builtin_bit_cast(uint32_t, y), power = max(bits & 0x7F800000u, 0x3C800000u);      // 2^-6 and up
+    const float f = __builtin_bit_cast(float, 0x80800000u - power), f2 = f * down;                              // 8 / power
+    const float n = floorf(y * f), w = v * f2 * f2;
+    const bool up = (float)r16 * __builtin_fmaf(n, 0x1p-15f, 0x1p-16f) < __builtin_fmaf(-n, n, w);              // (both products exact)
+    const int code = (int)((power >> 20) + (uint32_t)n) - 968 + (up ? 1 : 0);
+    return (uint32_t)min(max(code, (int)min(bits, 1u)), 126);       // (the largest finite one; above zero, not zero)
+}
+
+__device__ __forceinline__ void store_codes(uint8_t *codes, uint8_t *scale, const uint32_t (&word)[2], int e, int64_t at, int64_t count)
 {
     if (at + 8 <= count) {
         typedef uint32_t u2 __attribute__((ext_vector_type(2), aligned(1)));
-        u2 v;
-#pragma unroll
-        for (int i = 0; i < 2; ++i) v[i] = code[4 * i] | code[4 * i + 1] << 8 | code[4 * i + 2] << 16 | code[4 * i + 3] << 24;
-        *(u2 *)(codes + at) = v;
+        *(u2 *)(codes + at) = u2{word[0], word[1]};
     } else
         for (int i = 0; i < 8; ++i)
-            if (at + i < count) codes[at + i] = (uint8_t)code[i];
+            if (at + i < count) codes[at + i] = (uint8_t)(word[i / 4] >> (8 * (i & 3)));
     if ((threadIdx.x & 3) == 0 && at < count) scale[at / 32] = (uint8_t)(e + 127);
 }
 
@@ -218,8 +233,10 @@ __global__ __launch_bounds__(256) void adamw_step_kernel(AdamwPlan plan, int cop
         g[i] *= h.grad_scale;
         m[i] = m[i] * h.b1 + g[i] * h.a1;
         v[i] = v[i] * h.b2 + g[i] * g[i] * h.a2;
-        root[i] = sqrtf(v[i]);
-        p[i] = p[i] * keep - m[i] / (root[i] * h.rsqrt_c2 + h.eps) * h.step_size;
+        // root and quotient by the hardware's approximations, an ulp each: the update is lr times them, an ulp of it no ulp of p
+        root[i] = __builtin_amdgcn_sqrtf(v[i]);
+        const float by = m[i] * __builtin_amdgcn_rcpf(__builtin_fmaf(root[i], h.rsqrt_c2, h.eps));
+        p[i] = __builtin_fmaf(-by, h.step_size, p[i] * keep);
     }
     store8((P *)t.p, p, at, t.count);
     if (t.copy) {
@@ -232,32 +249,17 @@ __global__ __launch_bounds__(256) void adamw_step_kernel(AdamwPlan plan, int cop
         return;
     }
     const uint32_t key = adamw_mix(h.key + k);
-    float size[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) size[i] = fabsf(m[i]);
-    const int em = block_exponent(block_max(size)), ev = block_exponent(block_max(root));
+    const int em = block_exponent(block_max(m)), ev = block_exponent(block_max(root));
     const float down_m = power2(-em), down_v = power2(-ev);
-    uint32_t cm[8], cv[8];
+    uint32_t cm[2] = {0, 0}, cv[2] = {0, 0};
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
         const uint32_t r = adamw_mix((uint32_t)at + i + key);
-        const float rm = (float)(r & 0xFFFF) * 0x1p-16f, rv = (float)(r >> 16) * 0x1p-16f;
-        {
-            const float y = size[i] * down_m;
-            const int ey = max(exponent2(y), -6);
-            const int n = (int)fminf(y * power2(3 - ey) + rm, 16.f);
-            cm[i] = (uint32_t)min(((ey + 6) << 3) + n, 126) | (__builtin_bit_cast(uint32_t, m[i]) >> 31 << 7);
-        }
-        {
-            const float y = root[i] * down_v;
-            const int ey = max(exponent2(y), -6);
-            const float f = power2(3 - ey), f2 = f * down_v;
-            float n = floorf(y * f);
-            const float w = v[i] * f2 * f2;
-            n += rv * (2.f * n + 1.f) < w - n * n ? 1.f : 0.f;
-            if (v[i] > 0.f) n = fmaxf(n, 1.f);
-            cv[i] = (uint32_t)min(((ey + 6) << 3) + (int)fminf(n, 16.f), 126);
-        }
+        uint32_t &word = cm[i / 4];
+        const float y = m[i] * down_m;
+        word = (i & 3) == 0 ? first_code<0>(y, r << 16, word) : (i & 3) == 1 ? first_code<1>(y, r << 16, word)
+             : (i & 3) == 2 ? first_code<2>(y, r << 16, word) : first_code<3>(y, r << 16, word);
+        cv[i / 4] |= second_code(v[i], root[i], down_v, r >> 16) << (8 * (i & 3));
     }
     store_codes((uint8_t *)t.m, t.m_scale, cm, em, at, t.count);
     store_codes((uint8_t *)t.v, t.v_scale, cv, ev, at, t.count);
@@ -294,7 +296,7 @@ int flexadamw_plan_build(const flex_adamw_tensor *tensors, int n, int param_dtyp
     if (!tensors || !plan || !out) return FLEX_ERR_NULL;
     const size_t need = flexadamw_plan_bytes(tensors, n);
     if (need == 0 || !dtype_ok(param_dtype) || (state_bits != 8 && state_bits != 32) || (copy_dtype != FLEX_BF16 && copy_dtype != FLEX_F16) ||
-        !(beta1 >= 0. && beta1 < 1.) || !(beta2 >= 0. && beta2 < 1.) || !(eps > 0.) || steps < 0) return FLEX_ERR_SHAPE;
+        !(beta1 >= 0. && beta1 < 1.) || !(beta2 >= 0. && beta2 < 1.) || !((float)eps >= 1.17549435e-38f) || steps < 0) return FLEX_ERR_SHAPE;
     for (int i = 0; i < n; ++i)
         if (tensors[i].count > 0 && (!tensors[i].param || !tensors[i].exp_avg || !tensors[i].exp_avg_sq ||
                                      (state_bits == 8 && (!tensors[i].avg_scale || !tensors[i].avg_sq_scale)))) return FLEX_ERR_NULL;

@@ -208,7 +208,7 @@ __device__ __forceinline__ void row_sums(float &a, float &b, float (*place)[WAVE
 // PARAMS: with grad_w and grad_b (gx may be null then); otherwise only gx.
 // Threads of a workgroup: as many as find their registers (two sums and two rows' 16 bytes for each piece of U, and some 60 more).
 // us, 1024 and 512 threads, 252 MB of x, grad_out and grad_x: bf16, 2048 channels 97 and 114, 4096 (spilling at 1024) 110 and 101, fp32,
-// 2900 channels 106 and 101, 4096 175 and 101.
+// 3000 channels 106 and 101, 4096 175 and 101.
 constexpr int rows_bwd_threads(int L, int U, int N) { return L < 256 ? 256 : L > 256 || U * N <= 8 ? 1024 : 512; }
 template <class T, int L, int U, bool PARAMS, bool NARROW>
 __global__ __launch_bounds__(rows_bwd_threads(L, U, LANE_ELEMENTS<T>)) void norm_rows_bwd_kernel(const T *__restrict__ x, Param<T> w, const T *__restrict__ g,
