@@ -68,8 +68,7 @@ __device__ __forceinline__ bool ignored(const LogpArgs &a, int t) { return a.tar
 // ---- point-major, rows of up to 64 lanes' elements ------------------------------------------------------------------------
 // L lanes hold a row, U times 16 bytes each.  The best score is the maximum over the lanes, its class the smallest among those that
 // hold it; it is then taken out, and so on for each alternative: 2 log2 L steps and three operations an element each.
-// NARROW: rows of fewer classes than 16 bytes hold.
-template <class T, int L, int U, bool NARROW>
+template <class T, int L, int U>
 __global__ __launch_bounds__(256) void logp_rows_kernel(const T *__restrict__ x, LogpArgs a)
 {
     constexpr int N = LANE_ELEMENTS<T>;
@@ -84,20 +83,13 @@ __global__ __launch_bounds__(256) void logp_rows_kernel(const T *__restrict__ x,
 #pragma unroll
     for (int u = 0; u < U; ++u) {
         const int c0 = (u * L + sub) * N;
-        from[u] = NARROW ? c0 : Chunk<T>::from(c0, a.C);
+        from[u] = Chunk<T>::from(c0, a.C);
 #pragma unroll
         for (int j = 0; j < N; ++j) v[u][j] = -INFINITY;
-        if (skip) continue;
-        if (NARROW) {
-#pragma unroll
-            for (int j = 0; j < N; ++j)
-                if (c0 + j < a.C) v[u][j] = to_f32(at[c0 + j]);
-        } else
-            Chunk<T>::load(at + from[u], v[u]);
+        if (!skip) Chunk<T>::load(at + from[u], v[u]);
     }
-    if (!NARROW)
 #pragma unroll
-        for (int u = 0; u < U; ++u) Chunk<T>::mask(v[u], (u * L + sub) * N, a.C, -INFINITY);
+    for (int u = 0; u < U; ++u) Chunk<T>::mask(v[u], (u * L + sub) * N, a.C, -INFINITY);
     const float target_score = !skip && sub == 0 && a.target ? to_f32(at[t]) : 0.f;
     float best = -INFINITY;
 #pragma unroll
@@ -446,42 +438,71 @@ __global__ __launch_bounds__(64) void logp_join_kernel(const T *__restrict__ x, 
     for (int i = found + lane; i < a.top; i += 64) store_top(a, row * a.top + i, -INFINITY, NO_CLASS, k, log_s);
 }
 
-// ---- channel-major --------------------------------------------------------------------------------------------------------
+// ---- channel-major, and point-major rows of few classes ----------------------------------------------------------------------
 // A lane to a position, W waves of a workgroup share the classes: R of them a wave in registers, or (R = 0) any number, read again
 // for each alternative.  What the waves find meets in LDS.
-template <class T, int W, int R>
-__global__ __launch_bounds__(64 * W) void logp_cols_kernel(const T *__restrict__ x, LogpArgs a)
+// ROWS: point-major; the lanes of a wave read their rows 16 bytes at a time, which fills whole lines over a few loads.
+// A row of C <= R elements to a lane; what lies behind it is left as it is.
+template <class T, int R>
+__device__ __forceinline__ void load_few(const T *row, int C, float (&v)[R])
+{
+    constexpr int N = LANE_ELEMENTS<T>;
+#pragma unroll
+    for (int q = 0; q < R; q += N) {
+        if (q + N <= C) {
+            float piece[N];
+            Chunk<T>::load(row + q, piece);
+#pragma unroll
+            for (int j = 0; j < N; ++j) v[q + j] = piece[j];
+        } else
+#pragma unroll
+            for (int j = 0; j < N; ++j)
+                if (q + j < C) v[q + j] = to_f32(row[q + j]);
+    }
+}
+
+template <class T, int W, int R, bool ROWS>
+__global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void logp_lanes_kernel(const T *__restrict__ x, LogpArgs a)
 {
     __shared__ Sums s_sums[W][64];
     __shared__ float s_best[W][64];
     __shared__ int s_class[W][64];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const unsigned tiles = (unsigned)(a.N + 63) / 64;
-    const int64_t b = blockIdx.x / tiles;
-    const int n = (int)(blockIdx.x % tiles) * 64 + lane;
-    const bool mine = n < a.N;
+    const int lane = threadIdx.x & 63, wave = W == 1 ? 0 : threadIdx.x >> 6;
+    const unsigned tile = W == 1 ? blockIdx.x * 4 + (threadIdx.x >> 6) : blockIdx.x, tiles = ROWS ? 1u : (unsigned)(a.N + 63) / 64;
+    const int64_t b = ROWS ? 0 : tile / tiles;
+    const int64_t n = (int64_t)(ROWS ? tile : tile % tiles) * 64 + lane;
+    const bool mine = ROWS ? n < a.rows : n < a.N && b * a.N < a.rows;
     const int64_t row = b * a.N + n;
     const int t = mine && a.target ? a.target[row] : 0;
     const bool skip = !mine || ignored(a, t);
-    const T *at = x + b * a.C * a.stride + n;
+    const T *at = ROWS ? x + row * a.stride : x + b * a.C * a.stride + n;
+    const int64_t step = ROWS ? 1 : a.stride;
     const int per = R ? R : (a.C + W - 1) / W, first = wave * per, last = min(first + per, a.C);
     float v[R ? R : 1];
     Sums k{-INFINITY, 0.f, 0.f};
     float best = -INFINITY;
     if (R) {
 #pragma unroll
-        for (int i = 0; i < R; ++i) v[i] = !skip && first + i < last ? to_f32(at[(first + i) * a.stride]) : -INFINITY;
+        for (int i = 0; i < R; ++i) v[i] = -INFINITY;
+        if constexpr (ROWS) {
+            // (an ignored row's scores lie in lines that its neighbours need: they are loaded beside the target, and not used)
+            if (mine) load_few<T, R>(at, a.C, v);
+        } else
+#pragma unroll
+            for (int i = 0; i < R; ++i)
+                if (!skip && first + i < last) v[i] = to_f32(at[(first + i) * step]);
 #pragma unroll
         for (int i = 0; i < R; ++i) best = fmaxf(best, v[i]);
         k.m = best;
         const float m = centre(best);
 #pragma unroll
-        for (int i = 0; i < R; ++i) add_score(k, v[i], m);
+        for (int i = 0; i < R; ++i)
+            if (first + i / 4 * 4 < last) add_score(k, v[i], m);
     } else if (!skip) {
-        for (int c = first; c < last; ++c) best = fmaxf(best, to_f32(at[c * a.stride]));
+        for (int c = first; c < last; ++c) best = fmaxf(best, to_f32(at[c * step]));
         k.m = best;
         const float m = centre(best);
-        for (int c = first; c < last; ++c) add_score(k, to_f32(at[c * a.stride]), m);
+        for (int c = first; c < last; ++c) add_score(k, to_f32(at[c * step]), m);
     }
     if (W > 1) {
         s_sums[wave][lane] = k;
@@ -495,7 +516,7 @@ __global__ __launch_bounds__(64 * W) void logp_cols_kernel(const T *__restrict__
     const float log_s = logf(k.s);
     if (wave == 0 && mine) {
         if (skip) a.logp[row] = a.entropy[row] = a.lse[row] = 0.f;
-        else store_sums(a, row, a.target ? to_f32(at[t * a.stride]) : 0.f, k, log_s);
+        else store_sums(a, row, a.target ? to_f32(at[t * step]) : 0.f, k, log_s);
     }
     float last_best = INFINITY;
     int last_class = -1;
@@ -508,7 +529,7 @@ __global__ __launch_bounds__(64 * W) void logp_cols_kernel(const T *__restrict__
                 if (v[r] > best) { best = v[r]; c = first + r; }
         } else if (!skip) {
             for (int r = first; r < last; ++r) {
-                const float y = to_f32(at[r * a.stride]);
+                const float y = to_f32(at[r * step]);
                 if (y > best && (y < last_best || (y == last_best && r > last_class))) { best = y; c = r; }
             }
         }
@@ -523,7 +544,7 @@ __global__ __launch_bounds__(64 * W) void logp_cols_kernel(const T *__restrict__
                 if (s_best[w][lane] > best) { best = s_best[w][lane]; c = s_class[w][lane]; }
             __syncthreads();
         }
-        if (wave == 0 && mine) store_top(a, (b * a.top + i) * a.N + n, best, c, k, log_s);
+        if (wave == 0 && mine) store_top(a, ROWS ? row * a.top + i : (b * a.top + i) * a.N + n, skip ? -INFINITY : best, c, k, log_s);
         last_best = best;
         last_class = c;
         if (R)
@@ -592,6 +613,26 @@ __global__ __launch_bounds__(256) void logp_bwd_rows_kernel(const T *x, T *gx, L
     }
 }
 
+// Point-major rows of up to R classes, one to a lane.
+template <class T, int R>
+__global__ __launch_bounds__(256) void logp_bwd_few_kernel(const T *x, T *gx, LogpBwdArgs a)
+{
+    constexpr int N = LANE_ELEMENTS<T>;
+    const int64_t row = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (row >= a.rows) return;
+    T *to = gx + row * a.grad_stride;
+    float v[R];
+    load_few<T, R>(x + row * a.stride, a.C, v);
+    const LogpBwdRow f(a, row);
+#pragma unroll
+    for (int q = 0; q < R; q += N) {
+        float piece[N];
+#pragma unroll
+        for (int j = 0; j < N; ++j) piece[j] = f.zero ? 0.f : f(v[q + j], q + j);
+        if (q < a.C) Chunk<T>::store_row(to, q, a.C, piece);
+    }
+}
+
 // Channel-major: a lane to a position, a workgroup to 256 of them and 16 classes.
 constexpr int BWD_CLASSES = 16;
 template <class T>
@@ -648,16 +689,18 @@ static size_t parts_sums_bytes(int64_t rows, int parts) { return align256((size_
 template <class T>
 static hipError_t launch_logp_rows(const T *x, const LogpArgs &a, int dtype, void *ws, hipStream_t s)
 {
+    // A lane to a row up to 24 classes: us, four or eight lanes to a row and one, 2M rows, top 3: fp32, 13 classes 48 and 46, 17 classes
+    // 92 and 53, 24 classes 95 and 64, 32 classes 97 and 109; bf16, 17 classes 59 and 40, 24 classes 61 and 45.
+    if (a.C <= 24) {
+        const dim3 grid((unsigned)cdiv64(a.rows, 256));
+        if (a.C <= 16) hipLaunchKernelGGL((logp_lanes_kernel<T, 1, 16, true>), grid, dim3(256), 0, s, x, a);
+        else hipLaunchKernelGGL((logp_lanes_kernel<T, 1, 24, true>), grid, dim3(256), 0, s, x, a);
+        return hipGetLastError();
+    }
     if (a.C <= row_columns_max(dtype))
         return with_row_lanes<T>(a.C, [&](auto l, auto u) {
             constexpr int L = decltype(l)::value, U = decltype(u)::value;
-            const dim3 grid((unsigned)cdiv64(a.rows, 256 / L));
-            if constexpr (L == 4)
-                if (a.C < LANE_ELEMENTS<T>) {
-                    hipLaunchKernelGGL((logp_rows_kernel<T, L, U, true>), grid, dim3(256), 0, s, x, a);
-                    return hipGetLastError();
-                }
-            hipLaunchKernelGGL((logp_rows_kernel<T, L, U, false>), grid, dim3(256), 0, s, x, a);
+            hipLaunchKernelGGL((logp_rows_kernel<T, L, U>), dim3((unsigned)cdiv64(a.rows, 256 / L)), dim3(256), 0, s, x, a);
             return hipGetLastError();
         });
     const PartPlan q = plan_parts(a.rows, a.C, dtype);
@@ -671,12 +714,13 @@ static hipError_t launch_logp_rows(const T *x, const LogpArgs &a, int dtype, voi
 template <class T>
 static hipError_t launch_logp_cols(const T *x, const LogpArgs &a, int B, hipStream_t s)
 {
-    const dim3 grid((unsigned)(B * cdiv64(a.N, 64)));
-    if (a.C <= 16) hipLaunchKernelGGL((logp_cols_kernel<T, 1, 16>), grid, dim3(64), 0, s, x, a);
-    else if (a.C <= 32) hipLaunchKernelGGL((logp_cols_kernel<T, 2, 16>), grid, dim3(128), 0, s, x, a);
-    else if (a.C <= 64) hipLaunchKernelGGL((logp_cols_kernel<T, 4, 16>), grid, dim3(256), 0, s, x, a);
-    else if (a.C <= 128) hipLaunchKernelGGL((logp_cols_kernel<T, 8, 16>), grid, dim3(512), 0, s, x, a);
-    else hipLaunchKernelGGL((logp_cols_kernel<T, 16, 0>), grid, dim3(1024), 0, s, x, a);
+    const int64_t tiles = B * cdiv64(a.N, 64);
+    const dim3 grid((unsigned)tiles), four((unsigned)cdiv64(tiles, 4));
+    if (a.C <= 16) hipLaunchKernelGGL((logp_lanes_kernel<T, 1, 16, false>), four, dim3(256), 0, s, x, a);
+    else if (a.C <= 32) hipLaunchKernelGGL((logp_lanes_kernel<T, 2, 16, false>), grid, dim3(128), 0, s, x, a);
+    else if (a.C <= 64) hipLaunchKernelGGL((logp_lanes_kernel<T, 4, 16, false>), grid, dim3(256), 0, s, x, a);
+    else if (a.C <= 128) hipLaunchKernelGGL((logp_lanes_kernel<T, 8, 16, false>), grid, dim3(512), 0, s, x, a);
+    else hipLaunchKernelGGL((logp_lanes_kernel<T, 16, 0, false>), grid, dim3(1024), 0, s, x, a);
     return hipGetLastError();
 }
 
@@ -687,6 +731,13 @@ static hipError_t launch_logp_bwd(const T *x, T *gx, const LogpBwdArgs &a, int B
         const unsigned tiles = (unsigned)(a.N + 255) / 256, parts = (unsigned)(a.C + BWD_CLASSES - 1) / BWD_CLASSES;
         const int64_t grid = (int64_t)B * tiles * parts;
         hipLaunchKernelGGL(logp_bwd_cols_kernel<T>, dim3((unsigned)grid), dim3(256), 0, s, x, gx, a, tiles, parts);
+        return hipGetLastError();
+    }
+    // A lane to a row of at most 32 bytes: us, four lanes to a row and one, 2M rows: fp32, 2 classes 28 and 14, 8 classes 35 and 30,
+    // 13 classes 44 and 73; bf16, 5 classes 45 and 20, 13 classes 52 and 40, 24 classes 44 and 56.
+    constexpr int FEW = 32 / (int)sizeof(T);
+    if (a.C <= FEW) {
+        hipLaunchKernelGGL((logp_bwd_few_kernel<T, FEW>), dim3((unsigned)cdiv64(a.rows, 256)), dim3(256), 0, s, x, gx, a);
         return hipGetLastError();
     }
     if (a.C <= row_columns_max(dtype))
