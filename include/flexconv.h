@@ -410,7 +410,8 @@ int flex_validate_selection(const int32_t *sel, int B, int Ns, int Nf, int32_t *
  * The operators around a network's layers: layer norm, log probabilities of classes or tokens, optimizer step.
  * Their tensors are fp32, bf16 or fp16 (a flex_dtype), [B,C,N] or [B,N,C] by the layout flag; what they compute is computed in
  * fp32, and rounded once, to nearest, where it is stored.  Statistics, log probabilities and their gradients are fp32.
- * Any alignment of an element's size is taken.
+ * Any alignment of an element's size is taken.  A call has at most 2^31 - 1024 positions and as much work as one launch
+ * takes, 2^32 threads (tens of GB of a tensor); a larger one is refused as FLEX_ERR_SHAPE.
  */
 typedef enum { FLEX_F32 = 0, FLEX_BF16 = 1, FLEX_F16 = 2 } flex_dtype;
 
@@ -479,7 +480,7 @@ int flexlogp_bwd(const void *logits, const int32_t *target, const float *lse, co
  * holds the step's number, so that a captured step counts on in every replay; it fills *out, a handle of plain values for
  * flexadamw_step.  The plan is valid as long as the tensors stay where they are; calls that share one must be stream-ordered.
  * 0 <= beta1, beta2 < 1; eps a normal fp32 number.  `steps`: how many steps were done before (0 for a new run; the int64 at FLEX_ADAMW_STEPS_AT bytes of the plan is the count).
- *   tensors   host array of n (n <= 2^20); count < 2^31 elements, 0 allowed; no memory twice in the list
+ *   tensors   host array of n (n <= 2^20); count < 2^31 elements, 0 allowed, 2^35 in all; no memory twice in the list
  *   state_bits 32: exp_avg, exp_avg_sq fp32 [count].  8: e4m3 (OCP) bytes [count] and a power of two (e8m0 byte) for every 32 of
  *             them, [ceil(count / 32)]; exp_avg_sq holds roots: v = (value * scale)^2.  A state is rounded up or down at random so
  *             that its mean is exact (v in the square), by bits that depend on (seed, step, tensor, element) alone; a v above

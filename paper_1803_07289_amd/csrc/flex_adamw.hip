@@ -277,7 +277,7 @@ static bool adamw_list_ok(const flex_adamw_tensor *t, int n, int64_t *chunks)
         c += cdiv64(t[i].count, ADAMW_CHUNK);
     }
     *chunks = c;
-    return c < ((int64_t)1 << 31);
+    return one_launch(c * 256);
 }
 
 extern "C" {
@@ -335,7 +335,7 @@ int flexadamw_step(const flex_adamw *adamw, const void *const *grads, int n, int
 {
     if (!adamw || !adamw->plan || !grads) return FLEX_ERR_NULL;
     if (n != adamw->tensors || n <= 0 || !dtype_ok(grad_dtype) || !dtype_ok(adamw->param_dtype) ||
-        (adamw->state_bits != 8 && adamw->state_bits != 32) || adamw->chunks < 0 || adamw->chunks >= ((int64_t)1 << 31) || !isfinite(lr))
+        (adamw->state_bits != 8 && adamw->state_bits != 32) || adamw->chunks < 0 || !one_launch(adamw->chunks * 256) || !isfinite(lr))
         return FLEX_ERR_SHAPE;
     const AdamwPlan p = adamw_plan(adamw->plan, n);
     const hipStream_t s = (hipStream_t)stream;

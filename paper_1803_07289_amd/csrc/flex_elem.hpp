@@ -14,6 +14,10 @@ __device__ __forceinline__ float to_f32(T v) { return (float)v; }
 
 static inline bool dtype_ok(int d) { return d == FLEX_F32 || d == FLEX_BF16 || d == FLEX_F16; }
 static inline size_t dtype_bytes(int d) { return d == FLEX_F32 ? 4 : 2; }
+// Positions of a call: those of a last workgroup that lies past the end are numbered in an int too.
+static inline bool positions_ok(int B, int N) { return B > 0 && N > 0 && (int64_t)B * N <= INT32_MAX - 1023; }
+// A launch counts its threads in 32 bits.
+static inline bool one_launch(int64_t threads) { return threads < (int64_t)1 << 32; }
 
 // f(T{}) with the element type that a flex_dtype names
 template <class F>

@@ -255,7 +255,8 @@ __global__ __launch_bounds__(256) void logp_part_kernel(const T *__restrict__ x,
     request(begin);
     const float target_score = tid == 0 && a.target && p.parts == 1 ? to_f32(at[t]) : 0.f;
     Sums k{-INFINITY, 0.f, 0.f};       // of the lane; u in units of ln 2
-    float least = LOWEST, bound = LOWEST;       // what a candidate reaches; what `top` scores of the wave are known to reach
+    float least = LOWEST, bound = LOWEST;       // what a candidate reaches; what `top` scores of the part are known to reach
+    float last = -INFINITY;            // the least of the list when it was last cut
     int count = 0, renew = begin;      // the wave's list; where its bound is due
 
     // the list's best `top`, in order
@@ -268,7 +269,7 @@ __global__ __launch_bounds__(256) void logp_part_kernel(const T *__restrict__ x,
         if (count <= a.top) return;
         if (lane < a.top) list[lane] = s_cut[wave][lane];
         count = a.top;
-        const float last = score_of(s_cut[wave][a.top - 1]);
+        last = score_of(s_cut[wave][a.top - 1]);
         bound = fmaxf(bound, last);
         least = fmaxf(least, last);
         lds_in_order();
@@ -335,12 +336,8 @@ __global__ __launch_bounds__(256) void logp_part_kernel(const T *__restrict__ x,
         unsigned groups = 0;
 #pragma unroll
         for (int g = 0; g < GROUPS; ++g) groups |= most[g] >= least ? 1u << g : 0u;
-        bool was_cut = false;
         while (const uint64_t lanes = __ballot(groups != 0)) {
-            if (count + 4 * __popcll(lanes) > WAVE_LIST) {
-                cut();
-                was_cut = true;
-            }
+            if (count + 4 * __popcll(lanes) > WAVE_LIST) cut();
             const int g = groups ? __builtin_ctz(groups) : 0, own = c + (g / (N / 4) * 256 + tid) * N;
             const int from = Chunk<T>::from(own, a.C) + g % (N / 4) * 4;
             float w[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
@@ -355,7 +352,8 @@ __global__ __launch_bounds__(256) void logp_part_kernel(const T *__restrict__ x,
                 count += __popcll(mask);
             }
         }
-        if (was_cut) least = from_order_key(order_key(least) + 1);
+        // equal scores of later spans come after the list's (not after those of a wave that may be ahead, from which a larger bound is)
+        if (least == last) least = from_order_key(order_key(last) + 1);
     }
     if (count > LISTS_JOINED / 4) cut();
     Sums all{lanes_max<64>(k.m), 0.f, 0.f};
@@ -756,13 +754,26 @@ static hipError_t launch_logp_bwd(const T *x, T *gx, const LogpBwdArgs &a, int B
 
 using namespace flex;
 
+// Threads of a launch, at most: channel-major to 16 classes of a position, the waves of a workgroup being a power of two up to 16;
+// point-major to 16 bytes of a row, to 32 of one longer than 64 lanes hold.
+static int64_t logp_threads(int B, int N, int C, int dtype, int layout)
+{
+    if (layout == FLEX_LAYOUT_BCN) {
+        int64_t waves = 1;
+        while (waves < 16 && waves * 16 < C) waves *= 2;
+        return B * cdiv64(N, 256) * 256 * std::max(waves, cdiv64(C, BWD_CLASSES));
+    }
+    const int lane = 16 / (int)dtype_bytes(dtype);
+    int64_t threads = C <= row_columns_max(dtype) ? 4 : 256 * cdiv64(C, 256 * lane * 2);
+    while (threads < 64 && threads * lane < C) threads *= 2;
+    return (int64_t)B * N * threads;
+}
+
 static bool logp_sizes_ok(int B, int N, int C, int64_t row_stride, int dtype, int layout)
 {
-    return B > 0 && N > 0 && C > 0 && C <= FLEX_LOGP_MAX_CLASSES && (int64_t)B * N < ((int64_t)1 << 31) &&
-           (layout == FLEX_LAYOUT_BCN || layout == FLEX_LAYOUT_BNC) && dtype_ok(dtype) &&
-           row_stride >= (layout == FLEX_LAYOUT_BCN ? N : C) && row_stride < ((int64_t)1 << 31) &&
-           // workgroups of 4 KB of a row, or of 256 positions and 16 classes
-           (layout == FLEX_LAYOUT_BCN ? cdiv64(N, 256) * B * cdiv64(C, 16) : (int64_t)B * N * cdiv64(C, 1024)) < ((int64_t)1 << 31);
+    return positions_ok(B, N) && C > 0 && C <= FLEX_LOGP_MAX_CLASSES && (layout == FLEX_LAYOUT_BCN || layout == FLEX_LAYOUT_BNC) &&
+           dtype_ok(dtype) && row_stride >= (layout == FLEX_LAYOUT_BCN ? N : C) && row_stride < ((int64_t)1 << 31) &&
+           one_launch(logp_threads(B, N, C, dtype, layout));
 }
 
 extern "C" {

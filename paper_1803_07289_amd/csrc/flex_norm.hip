@@ -695,6 +695,25 @@ static void with_col_waves(int C, F f)
     else f(std::integral_constant<int, 16>{});
 }
 
+// Rows that a group of the forward pass takes together
+constexpr int rows_together(int L, int U) { return L <= 64 && U == 1 ? 4 : L == 64 ? 2 : 1; }
+
+// Threads of a launch that has some for every position, at most
+static int64_t norm_threads(int B, int N, int C, int dtype, bool bcn)
+{
+    if (bcn) {
+        int64_t waves = 16;
+        if (C <= COL_CHANNELS_MAX) with_col_waves(C, [&](auto w) { waves = decltype(w)::value; });
+        return B * cdiv64(N, 64) * 64 * waves;
+    }
+    int64_t threads = 1024;
+    const auto of_row = [&](auto l, auto u) { threads = decltype(l)::value / rows_together(decltype(l)::value, decltype(u)::value); };
+    if (dtype == FLEX_F32) with_row_threads<float>(C, of_row);
+    else with_row_threads<bf16>(C, of_row);
+    return (int64_t)B * N * threads;
+}
+constexpr int64_t WALKERS = 1 << 20;        // workgroups, at most, of those backward kernels that walk over the positions
+
 // Partial sums of grad_w and grad_b: the workgroups that walk over the positions, four turns at least to each.
 static int norm_slices(int B, int N, int C, int dtype, bool bcn)
 {
@@ -730,7 +749,7 @@ static hipError_t launch_norm_fwd(const T *x, const void *weight, const void *bi
         return hipGetLastError();
     }
     if (!with_row_threads<T>(C, [&](auto l, auto u) {
-            constexpr int L = decltype(l)::value, U = decltype(u)::value, R = L <= 64 && U == 1 ? 4 : L == 64 ? 2 : 1;
+            constexpr int L = decltype(l)::value, U = decltype(u)::value, R = rows_together(L, U);
             const dim3 grid((unsigned)cdiv64(rows, (int64_t)std::max(256 / L, 1) * R)), wg(std::max(L, 256));
             if constexpr (L == 4)
                 if (C < LANE_ELEMENTS<T>) {
@@ -755,7 +774,7 @@ static hipError_t launch_norm_bwd(const T *x, const void *weight, const T *g, co
         with_col_waves(C, [&](auto waves) {
             constexpr int W = decltype(waves)::value;
             if (gw) hipLaunchKernelGGL((norm_cols_bwd_kernel<T, W, true>), dim3((unsigned)slices), dim3(64 * W), 0, s, x, w, g, mean, rstd, gx, partials, N, C, tiles, total);
-            else hipLaunchKernelGGL((norm_cols_bwd_kernel<T, W, false>), dim3(total), dim3(64 * W), 0, s, x, w, g, mean, rstd, gx, partials, N, C, tiles, total);
+            else hipLaunchKernelGGL((norm_cols_bwd_kernel<T, W, false>), dim3((unsigned)std::min<int64_t>(total, WALKERS)), dim3(64 * W), 0, s, x, w, g, mean, rstd, gx, partials, N, C, tiles, total);
         });
     } else if (bcn) {
         if (gx) hipLaunchKernelGGL(norm_many_cols_bwd_kernel<T>, dim3((unsigned)(B * cdiv64(N, 64))), dim3(1024), 0, s, x, w, g, mean, rstd, gx, N, C);
@@ -765,7 +784,7 @@ static hipError_t launch_norm_bwd(const T *x, const void *weight, const T *g, co
     } else if (!with_row_threads<T>(C, [&](auto l, auto u) {
                    constexpr int L = decltype(l)::value, U = decltype(u)::value;
                    constexpr int WG = rows_bwd_threads(L, U, LANE_ELEMENTS<T>);
-                   const dim3 wg(WG), grid((unsigned)(gw ? slices : cdiv64(rows, WG / L)));
+                   const dim3 wg(WG), grid((unsigned)(gw ? slices : std::min(cdiv64(rows, WG / L), WALKERS)));
                    auto launch = [&](auto params, auto narrow) {
                        hipLaunchKernelGGL((norm_rows_bwd_kernel<T, L, U, decltype(params)::value, decltype(narrow)::value>), grid, wg, 0, s, x,
                                           w, g, mean, rstd, gx, partials, rows, C);
@@ -795,8 +814,9 @@ using namespace flex;
 
 static bool norm_sizes_ok(int B, int N, int C, int layout, int dtype, int param_dtype)
 {
-    return B > 0 && N > 0 && C > 0 && C <= FLEX_NORM_MAX_CHANNELS && (int64_t)B * N < ((int64_t)1 << 31) &&
-           (layout == FLEX_LAYOUT_BCN || layout == FLEX_LAYOUT_BNC) && dtype_ok(dtype) && (param_dtype == FLEX_F32 || param_dtype == dtype);
+    return positions_ok(B, N) && C > 0 && C <= FLEX_NORM_MAX_CHANNELS && (layout == FLEX_LAYOUT_BCN || layout == FLEX_LAYOUT_BNC) &&
+           dtype_ok(dtype) && (param_dtype == FLEX_F32 || param_dtype == dtype) &&
+           one_launch(norm_threads(B, N, C, dtype, layout == FLEX_LAYOUT_BCN));
 }
 
 extern "C" {

@@ -141,6 +141,28 @@ def test_rows_that_are_all_alike_take_the_lowest_classes(C, dtype, layout):
 
 
 @pytest.mark.parametrize("layout", [fx.BNC, fx.BCN], ids=["bnc", "bcn"])
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("C, rows, times", [(6, 300, 1), (30, 300, 1), (300, 300, 1), (2500, 40, 1), (9000, 40, 30), (66000, 3, 1),
+                                            (66000, 12, 25), (66000, 12, 200)])
+def test_scores_of_few_values(C, rows, times, dtype, layout):
+    """Coarse scores: the last alternative is one of many equals wherever they lie, and zeros of both signs are equal.  The same rows
+    many times over, so that a row is one workgroup's: the same results."""
+    rng = np.random.default_rng(C + rows)
+    x = np.round(rng.standard_normal((rows, C)) * 2) / 2
+    x[::3] = np.minimum(x[::3], 0.0)                                  # zeros are the best ones
+    x = np.where((x == 0) & (rng.random((rows, C)) < 0.5), -0.0, x)
+    x[1::3] += np.sort(np.round(rng.random(C) * 4))                   # better ones keep coming
+    top = min(C, 32)
+    dx = laid_out(x, 1, layout, TYPES[dtype])
+    assert bool(torch.signbit(dx[dx == 0]).any())
+    check_fwd(x, None, fx.flexlogp_fwd(dx, top=top, layout=layout), top, layout)
+    if times > 1:
+        many = [v.double() for v in fx.flexlogp_fwd(dx.repeat(times, 1, 1), top=top, layout=layout)[1:]]
+        check_fwd(x, None, [None] + [v[:1] for v in many], top, layout)
+        assert all(torch.equal(v, v[:1].expand_as(v)) for v in many)
+
+
+@pytest.mark.parametrize("layout", [fx.BNC, fx.BCN], ids=["bnc", "bcn"])
 @pytest.mark.parametrize("C", [9, 300, 3000, 70000])
 def test_nan_and_infinity_among_the_scores(C, layout):
     _, x = scores(4, 4, C, torch.float32)
