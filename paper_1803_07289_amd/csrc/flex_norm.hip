@@ -38,6 +38,23 @@ __device__ __forceinline__ float row_sum(float v, float *place)
     return v;
 }
 
+// what lane i has, on all of them
+__device__ __forceinline__ float lane_value(float v, int i)
+{
+    return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), i));
+}
+
+// Sums of columns c0 .. of C: x holds the columns from Chunk::from(c0, C) on, those before c0 another lane's.
+template <int N>
+__device__ __forceinline__ void store_columns(float *to, int c0, int C, const float (&x)[N])
+{
+    if (c0 + N <= C) Chunk<float, N>::store(to + c0, x);
+    else
+#pragma unroll
+        for (int j = 0; j < N; ++j)
+            if (C - N + j >= c0) to[C - N + j] = x[j];
+}
+
 // ---- point-major ------------------------------------------------------------------------------------------------------------
 // L threads hold a row, U times 16 bytes each; a group of them takes R rows, which it asks for together.  NARROW: rows of fewer
 // channels than 16 bytes hold.
@@ -198,26 +215,23 @@ __device__ __forceinline__ void row_sums(float &a, float &b, float (*place)[WAVE
     }
 }
 
-// Backward: groups of L threads walk over rows, the next row of each on its way, their columns' shares of grad_w and grad_b in
-// registers; those of a workgroup's groups are added up at the end: one partial sum of 2 C a workgroup, and one workgroup to a
-// compute unit where rows take 256 threads or more (8188 x 5120 bf16: 256 partial sums are 10 MB, of the 252 that have to move).
+// Backward: groups of L threads (lanes of a wave, or 1024) walk over rows, the next row of each on its way, their columns' shares of
+// grad_w and grad_b in registers; those of a workgroup's groups are added up at the end: one partial sum of 2 C a workgroup.
 // A row stays as it was read and is converted twice, for its two sums and for its results: half the registers.  The weights are in
 // LDS where rows are long: read from memory they would queue behind the next row.  No store is in a branch: a wait for the next
 // row could not be told from one for the store then.  Lanes past a row's end and groups past the last row store what another one
 // stores too, the same values.
 // PARAMS: with grad_w and grad_b (gx may be null then); otherwise only gx.
-// Threads of a workgroup: as many as find their registers (two sums and two rows' 16 bytes for each piece of U, and some 60 more).
-// us, 1024 and 512 threads, 252 MB of x, grad_out and grad_x: bf16, 2048 channels 97 and 114, 4096 (spilling at 1024) 110 and 101, fp32,
-// 3000 channels 106 and 101, 4096 175 and 101.
-constexpr int rows_bwd_threads(int L, int U, int N) { return L < 256 ? 256 : L > 256 || U * N <= 8 ? 1024 : 512; }
+// Measured with x, grad_out and grad_x of 504 MB: bf16, 64 channels 109 us (4.6 TB/s), 512 104 us, 16384 110 us; fp32, 64 channels 100 us.
+constexpr int rows_bwd_threads(int L) { return L > 256 ? L : 256; }
 template <class T, int L, int U, bool PARAMS, bool NARROW>
-__global__ __launch_bounds__(rows_bwd_threads(L, U, LANE_ELEMENTS<T>)) void norm_rows_bwd_kernel(const T *__restrict__ x, Param<T> w, const T *__restrict__ g,
+__global__ __launch_bounds__(rows_bwd_threads(L)) void norm_rows_bwd_kernel(const T *__restrict__ x, Param<T> w, const T *__restrict__ g,
                                                                             const float *__restrict__ mean, const float *__restrict__ rstd,
                                                                             T *__restrict__ gx, float *__restrict__ partials,
                                                                             int64_t rows, int C)
 {
-    constexpr int N = LANE_ELEMENTS<T>, WG = rows_bwd_threads(L, U, N), G = WG / L;
-    constexpr bool SHARED = L >= 256;
+    constexpr int N = LANE_ELEMENTS<T>, WG = rows_bwd_threads(L), G = WG / L;
+    constexpr bool SHARED = L > 64;
     typedef typename Chunk<T>::V V;
     __shared__ float s_place[2][2][WG / 64];
     __shared__ __attribute__((aligned(16))) float s_weight[SHARED ? L * U * N : 1];
@@ -391,13 +405,132 @@ __global__ __launch_bounds__(rows_bwd_threads(L, U, LANE_ELEMENTS<T>)) void norm
                     for (int j = 0; j < N; ++j) acc[u][j] += s_sum[(k * U * N + u * N + j) * L + sub];
 #pragma unroll
             for (int u = 0; u < U; ++u) {
-                const int c0 = (u * L + sub) * N, from = NARROW ? c0 : Chunk<T>::from(c0, C);
-#pragma unroll
-                for (int j = 0; j < N; ++j)
-                    if (from + j >= c0 && from + j < C) to[which * C + from + j] = acc[u][j];
+                const int c0 = (u * L + sub) * N;
+                if (NARROW) Chunk<float, N>::store_row(to + which * C, c0, C, acc[u]);
+                else if (c0 < C) store_columns(to + which * C, c0, C, acc[u]);
             }
         }
         if (GG > 1) __syncthreads();
+    }
+}
+
+// Backward of rows that take W waves of 16 bytes a lane (2 to 16): as many groups of W waves in a workgroup as 16 waves make, D rows
+// of each group in registers, all but one of them on their way.  With grad_w and grad_b one workgroup to a compute unit, since each
+// leaves a partial sum (8188 x 5120 bf16: 10 MB of them beside the 252 MB that have to move; two workgroups 7 us more), without
+// at least two.  A wave's vector operations decide beside the memory, 14 an element: nothing in a turn is chosen by a lane's place, what
+// is another lane's has weight 0 in the row's sums and is left out when the parameters' are stored.
+// 8188 x 5120 bf16: 46 us with the 4 us of the partial sums' sum (5.5 TB/s; adding x and grad_out 44), without the parameters' 42.
+// x, grad_out and grad_x of 504 MB: bf16, 1000 channels 109 us (rows not on 16 bytes), 2048 97, 8192 101; fp32, 1024 channels 95, 4096 97.
+template <class T, bool PARAMS, bool GRAD_X, int D>
+__global__ __launch_bounds__(1024) void norm_wide_rows_bwd_kernel(const T *__restrict__ x, Param<T> w, const T *__restrict__ g,
+                                                                  const float *__restrict__ mean, const float *__restrict__ rstd,
+                                                                  T *__restrict__ gx, float *__restrict__ partials, int64_t rows, int C,
+                                                                  int W)
+{
+    constexpr int N = LANE_ELEMENTS<T>;
+    typedef typename Chunk<T>::V V;
+    __shared__ float s_place[2][2][16], s_sum[PARAMS ? 1024 * N : 1];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), G = (int)(blockDim.x >> 6) / W;
+    const int group = wave / W, sub = (int)threadIdx.x - group * W * 64, c0 = sub * N;
+    const unsigned from = (unsigned)Chunk<T>::from(c0, C);
+    const float part = 1.f / (float)C;
+    const int64_t step = (int64_t)gridDim.x * G;
+    int zero;       // (in a vector register: a row's statistics come behind its elements, not through the scalar cache, which LDS waits for)
+    asm("v_mov_b32 %0, 0" : "=v"(zero));
+    struct Row {
+        Words x, g;
+        float mean, rstd;
+    } ring[D];
+    auto request = [&](Row &to, int64_t first) {
+        const int64_t row = min(first + group, rows - 1);
+        to.x = __builtin_bit_cast(Words, *(const V *)(x + row * C + from));
+        to.g = __builtin_bit_cast(Words, *(const V *)(g + row * C + from));
+        to.mean = (mean + row)[zero];
+        to.rstd = (rstd + row)[zero];
+    };
+    // weights, and those in the row's sums: a lane that reads at the row's end has another lane's columns too, whose sums are that one's
+    float ww[N], own[N], gw[N], gb[N];
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+        ww[j] = 1.f;
+        gw[j] = gb[j] = 0.f;
+    }
+    if (w.p) w.load(from, ww);
+#pragma unroll
+    for (int j = 0; j < N; ++j) own[j] = (int)from + j < c0 ? 0.f : ww[j];
+    int64_t first = (int64_t)blockIdx.x * G;
+#pragma unroll
+    for (int d = 0; d < D - 1; ++d) request(ring[d], first + d * step);
+    int turn = 0;
+    auto take = [&](const Row &now, int64_t first) {
+        float xx[N], gg[N];
+        unpack<T>(now.x, xx);
+        unpack<T>(now.g, gg);
+#pragma unroll
+        for (int j = 0; j < N; ++j) xx[j] = (xx[j] - now.mean) * now.rstd;
+        if (GRAD_X) {
+            float s1 = 0.f, s2 = 0.f;
+#pragma unroll
+            for (int j = 0; j < N; ++j) {
+                const float h = gg[j] * own[j];
+                s1 += h;
+                s2 = __builtin_fmaf(h, xx[j], s2);
+            }
+            s1 = lanes_sum<64>(s1);
+            s2 = lanes_sum<64>(s2);
+            if (lane == 0) {
+                s_place[turn][0][wave] = s1;
+                s_place[turn][1][wave] = s2;
+            }
+            __syncthreads();
+            const int from_wave = group * W + min(lane, W - 1);
+            s1 = s_place[turn][0][from_wave];
+            s2 = s_place[turn][1][from_wave];
+            turn ^= 1;
+            s1 = lane_value(lanes_sum<16>(lane < W ? s1 : 0.f), 0) * part;
+            s2 = lane_value(lanes_sum<16>(lane < W ? s2 : 0.f), 0) * part;
+            // (a group past the last row stores what another one stores too, the same values: no store in a branch)
+            T *const to = gx + min(first + group, rows - 1) * C;
+            float out[N];
+#pragma unroll
+            for (int j = 0; j < N; ++j) out[j] = __builtin_fmaf(-xx[j], s2, __builtin_fmaf(gg[j], ww[j], -s1)) * now.rstd;
+            Chunk<T>::store(to + from, out);
+        }
+        if (PARAMS && first + group < rows)
+#pragma unroll
+            for (int j = 0; j < N; ++j) {
+                gw[j] = __builtin_fmaf(gg[j], xx[j], gw[j]);
+                gb[j] += gg[j];
+            }
+    };
+    for (bool more = true; more;)
+#pragma unroll
+        for (int d = 0; d < D; ++d) {
+            request(ring[(d + D - 1) % D], first + (D - 1) * step);        // (behind the last row: the last one again)
+            take(ring[d], first);
+            if ((first += step) >= rows) {
+                more = false;
+                break;
+            }
+        }
+    if (!PARAMS) return;
+    float *const to = partials + (int64_t)blockIdx.x * 2 * C;
+#pragma unroll
+    for (int which = 0; which < 2; ++which) {
+        float (&acc)[N] = which ? gb : gw;
+        if (G > 1) {
+            __syncthreads();
+            if (group > 0)
+#pragma unroll
+                for (int j = 0; j < N; ++j) s_sum[((group - 1) * N + j) * W * 64 + sub] = acc[j];
+            __syncthreads();
+        }
+        if (group == 0) {
+            for (int k = 0; k < G - 1; ++k)
+#pragma unroll
+                for (int j = 0; j < N; ++j) acc[j] += s_sum[(k * N + j) * W * 64 + sub];
+            if (c0 < C) store_columns(to + which * C, c0, C, acc);
+        }
     }
 }
 
@@ -458,12 +591,6 @@ __device__ __forceinline__ float waves_sum(float v, float (*place)[64])
 #pragma unroll
     for (int i = 1; i < W; ++i) v += place[i][lane];
     return v;
-}
-
-// what lane i has, on all of them (a channel's weight: one load for R of them)
-__device__ __forceinline__ float lane_value(float v, int i)
-{
-    return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), i));
 }
 
 template <class T, int W, int R>
@@ -637,22 +764,25 @@ __global__ __launch_bounds__(256) void norm_many_cols_params_kernel(const T *__r
 }
 
 // ---- partial sums to gradients ------------------------------------------------------------------------------------------------
-// 16 columns to a workgroup, 16 threads to a column, in the same order at every call.
-__global__ __launch_bounds__(256) void norm_params_sum_kernel(const float *__restrict__ partials, int slices, void *gw, void *gb, int C,
-                                                              int pdtype)
+// COLUMNS to a workgroup, 1024 / COLUMNS threads to each, in the same order at every call: 64, which lines are read whole for, where
+// that makes 64 workgroups, otherwise 16.
+template <int COLUMNS>
+__global__ __launch_bounds__(1024) void norm_params_sum_kernel(const float *__restrict__ partials, int slices, void *gw, void *gb, int C,
+                                                               int pdtype)
 {
-    __shared__ float s_sum[16][17];
-    const int column = blockIdx.x * 16 + (threadIdx.x & 15), slot = threadIdx.x >> 4;
+    __shared__ float s_sum[16][COLUMNS];
+    const int own = threadIdx.x % COLUMNS, column = blockIdx.x * COLUMNS + own;
     float sum = 0.f;
     if (column < 2 * C)
-#pragma unroll 8
-        for (int i = slot; i < slices; i += 16) sum += partials[(int64_t)i * 2 * C + column];
-    s_sum[slot][threadIdx.x & 15] = sum;
+#pragma unroll 16
+        for (int i = threadIdx.x / COLUMNS; i < slices; i += 1024 / COLUMNS) sum += partials[(int64_t)i * 2 * C + column];
+    for (int o = COLUMNS; o < 64; o <<= 1) sum += __shfl_xor(sum, o);
+    s_sum[threadIdx.x >> 6][own] = sum;
     __syncthreads();
-    if (slot != 0 || column >= 2 * C) return;
-    sum = s_sum[0][threadIdx.x];
+    if (threadIdx.x >= COLUMNS || column >= 2 * C) return;
+    sum = s_sum[0][own];
 #pragma unroll
-    for (int i = 1; i < 16; ++i) sum += s_sum[i][threadIdx.x];
+    for (int i = 1; i < 16; ++i) sum += s_sum[i][own];
     if (column < C) store_param(gw, pdtype, column, sum);
     else store_param(gb, pdtype, column - C, sum);
 }
@@ -695,6 +825,10 @@ static void with_col_waves(int C, F f)
     else f(std::integral_constant<int, 16>{});
 }
 
+// Rows of two to sixteen waves of 16 bytes a lane: the backward pass has a kernel for them.
+static bool wide_rows(int C, int lane) { return C > 64 * lane && C <= 1024 * lane; }
+static int wide_waves(int C, int lane) { return (C + 64 * lane - 1) / (64 * lane); }
+
 // Rows that a group of the forward pass takes together
 constexpr int rows_together(int L, int U) { return L <= 64 && U == 1 ? 4 : L == 64 ? 2 : 1; }
 
@@ -725,10 +859,10 @@ static int norm_slices(int B, int N, int C, int dtype, bool bcn)
     }
     if (C > ROW_CHANNELS_MAX) return (int)std::min<int64_t>(64, cdiv64(rows, 16));
     const int lane = 16 / (int)dtype_bytes(dtype);
-    int groups = C <= 256 * 4 * lane ? 2 : 1;
+    int groups = wide_rows(C, lane) ? 16 / wide_waves(C, lane) : 1;
     for (const int L : {64, 32, 16, 8, 4})
-        if (C <= (L == 64 ? 128 : L) * lane) groups = 256 / L;
-    return (int)std::max<int64_t>(1, std::min<int64_t>(cdiv64(rows, 4 * groups), C <= 128 * lane ? 4 * cus : cus));
+        if (C <= L * lane) groups = 256 / L;
+    return (int)std::max<int64_t>(1, std::min<int64_t>(cdiv64(rows, 4 * groups), C <= 64 * lane ? 4 * cus : cus));
 }
 
 template <class T>
@@ -781,9 +915,17 @@ static hipError_t launch_norm_bwd(const T *x, const void *weight, const T *g, co
         if (gw)
             hipLaunchKernelGGL(norm_many_cols_params_kernel<T>, dim3((unsigned)C, (unsigned)slices), dim3(256), 0, s, x, g, mean, rstd,
                                partials, rows, cdiv64(rows, slices), N, C);
+    } else if (wide_rows(C, LANE_ELEMENTS<T>)) {
+        const int W = wide_waves(C, LANE_ELEMENTS<T>), groups = 16 / W;
+        const int64_t walkers = std::min(cdiv64(rows, groups), std::max<int64_t>(2 * device_cu_count(), cdiv64(rows, 16 * groups)));
+        const dim3 wg(64 * W * groups), grid((unsigned)(gw ? slices : std::min(walkers, WALKERS)));
+        if (!gw) hipLaunchKernelGGL((norm_wide_rows_bwd_kernel<T, false, true, 2>), grid, wg, 0, s, x, w, g, mean, rstd, gx, partials, rows, C, W);
+        else if (gx) hipLaunchKernelGGL((norm_wide_rows_bwd_kernel<T, true, true, 3>), grid, wg, 0, s, x, w, g, mean, rstd, gx, partials, rows, C, W);
+        else hipLaunchKernelGGL((norm_wide_rows_bwd_kernel<T, true, false, 3>), grid, wg, 0, s, x, w, g, mean, rstd, gx, partials, rows, C, W);
     } else if (!with_row_threads<T>(C, [&](auto l, auto u) {
                    constexpr int L = decltype(l)::value, U = decltype(u)::value;
-                   constexpr int WG = rows_bwd_threads(L, U, LANE_ELEMENTS<T>);
+                   if constexpr (L <= 64 ? U == 1 : L == 1024) {
+                   constexpr int WG = rows_bwd_threads(L);
                    const dim3 wg(WG), grid((unsigned)(gw ? slices : std::min(cdiv64(rows, WG / L), WALKERS)));
                    auto launch = [&](auto params, auto narrow) {
                        hipLaunchKernelGGL((norm_rows_bwd_kernel<T, L, U, decltype(params)::value, decltype(narrow)::value>), grid, wg, 0, s, x,
@@ -797,14 +939,17 @@ static hipError_t launch_norm_bwd(const T *x, const void *weight, const T *g, co
                        }
                    if (gw) launch(std::true_type{}, std::false_type{});
                    else launch(std::false_type{}, std::false_type{});
+                   }
                })) {
         if (gx) hipLaunchKernelGGL(norm_long_rows_bwd_kernel<T>, dim3((unsigned)rows), dim3(1024), 0, s, x, w, g, mean, rstd, gx, C);
         if (gw)
             hipLaunchKernelGGL(norm_long_rows_params_kernel<T>, dim3((unsigned)((C + 255) / 256), (unsigned)slices), dim3(256), 0, s, x, g,
                                mean, rstd, partials, rows, cdiv64(rows, slices), C);
     }
-    if (gw)
-        hipLaunchKernelGGL(norm_params_sum_kernel, dim3((unsigned)((2 * (int64_t)C + 15) / 16)), dim3(256), 0, s, partials, slices, gw, gb, C, pdtype);
+    if (gw) {
+        if (2 * C >= 64 * 64) hipLaunchKernelGGL(norm_params_sum_kernel<64>, dim3((unsigned)(2 * C + 63) / 64), dim3(1024), 0, s, partials, slices, gw, gb, C, pdtype);
+        else hipLaunchKernelGGL(norm_params_sum_kernel<16>, dim3((unsigned)(2 * C + 15) / 16), dim3(1024), 0, s, partials, slices, gw, gb, C, pdtype);
+    }
     return hipGetLastError();
 }
 
