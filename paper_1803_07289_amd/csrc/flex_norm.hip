@@ -215,14 +215,14 @@ __device__ __forceinline__ void row_sums(float &a, float &b, float (*place)[WAVE
     }
 }
 
-// Backward: groups of L threads (lanes of a wave, or 1024) walk over rows, the next row of each on its way, their columns' shares of
+// Backward: groups of L threads (up to 32, or 1024) walk over rows, the next row of each on its way, their columns' shares of
 // grad_w and grad_b in registers; those of a workgroup's groups are added up at the end: one partial sum of 2 C a workgroup.
 // A row stays as it was read and is converted twice, for its two sums and for its results: half the registers.  The weights are in
 // LDS where rows are long: read from memory they would queue behind the next row.  No store is in a branch: a wait for the next
 // row could not be told from one for the store then.  Lanes past a row's end and groups past the last row store what another one
 // stores too, the same values.
 // PARAMS: with grad_w and grad_b (gx may be null then); otherwise only gx.
-// Measured with x, grad_out and grad_x of 504 MB: bf16, 64 channels 109 us (4.6 TB/s), 512 104 us, 16384 110 us; fp32, 64 channels 100 us.
+// Measured with x, grad_out and grad_x of 504 MB: bf16, 64 channels 105 us (4.8 TB/s), 128 104, 16384 110; fp32, 64 channels 100.
 constexpr int rows_bwd_threads(int L) { return L > 256 ? L : 256; }
 template <class T, int L, int U, bool PARAMS, bool NARROW>
 __global__ __launch_bounds__(rows_bwd_threads(L)) void norm_rows_bwd_kernel(const T *__restrict__ x, Param<T> w, const T *__restrict__ g,
@@ -414,13 +414,14 @@ __global__ __launch_bounds__(rows_bwd_threads(L)) void norm_rows_bwd_kernel(cons
     }
 }
 
-// Backward of rows that take W waves of 16 bytes a lane (2 to 16): as many groups of W waves in a workgroup as 16 waves make, D rows
+// Backward of rows that take W waves of 16 bytes a lane (1 to 16): as many groups of W waves in a workgroup as 16 waves make, D rows
 // of each group in registers, all but one of them on their way.  With grad_w and grad_b one workgroup to a compute unit, since each
 // leaves a partial sum (8188 x 5120 bf16: 10 MB of them beside the 252 MB that have to move; two workgroups 7 us more), without
 // at least two.  A wave's vector operations decide beside the memory, 14 an element: nothing in a turn is chosen by a lane's place, what
 // is another lane's has weight 0 in the row's sums and is left out when the parameters' are stored.
 // 8188 x 5120 bf16: 46 us with the 4 us of the partial sums' sum (5.5 TB/s; adding x and grad_out 44), without the parameters' 42.
-// x, grad_out and grad_x of 504 MB: bf16, 1000 channels 109 us (rows not on 16 bytes), 2048 97, 8192 101; fp32, 1024 channels 95, 4096 97.
+// x, grad_out and grad_x of 504 MB: bf16, 264 channels 107 us (33 of 64 lanes), 512 98, 1000 100 (every other row off 16 bytes), 2048 97,
+// 8192 101; fp32, 132 channels 96, 1024 95, 4096 97.
 template <class T, bool PARAMS, bool GRAD_X, int D>
 __global__ __launch_bounds__(1024) void norm_wide_rows_bwd_kernel(const T *__restrict__ x, Param<T> w, const T *__restrict__ g,
                                                                   const float *__restrict__ mean, const float *__restrict__ rstd,
@@ -825,8 +826,8 @@ static void with_col_waves(int C, F f)
     else f(std::integral_constant<int, 16>{});
 }
 
-// Rows of two to sixteen waves of 16 bytes a lane: the backward pass has a kernel for them.
-static bool wide_rows(int C, int lane) { return C > 64 * lane && C <= 1024 * lane; }
+// Rows of more than 32 lanes of 16 bytes, up to 16 waves: the backward pass has a kernel for them.
+static bool wide_rows(int C, int lane) { return C > 32 * lane && C <= 1024 * lane; }
 static int wide_waves(int C, int lane) { return (C + 64 * lane - 1) / (64 * lane); }
 
 // Rows that a group of the forward pass takes together
@@ -860,9 +861,9 @@ static int norm_slices(int B, int N, int C, int dtype, bool bcn)
     if (C > ROW_CHANNELS_MAX) return (int)std::min<int64_t>(64, cdiv64(rows, 16));
     const int lane = 16 / (int)dtype_bytes(dtype);
     int groups = wide_rows(C, lane) ? 16 / wide_waves(C, lane) : 1;
-    for (const int L : {64, 32, 16, 8, 4})
+    for (const int L : {32, 16, 8, 4})
         if (C <= L * lane) groups = 256 / L;
-    return (int)std::max<int64_t>(1, std::min<int64_t>(cdiv64(rows, 4 * groups), C <= 64 * lane ? 4 * cus : cus));
+    return (int)std::max<int64_t>(1, std::min<int64_t>(cdiv64(rows, 4 * groups), C <= 32 * lane ? 4 * cus : cus));
 }
 
 template <class T>
@@ -924,7 +925,7 @@ static hipError_t launch_norm_bwd(const T *x, const void *weight, const T *g, co
         else hipLaunchKernelGGL((norm_wide_rows_bwd_kernel<T, true, false, 3>), grid, wg, 0, s, x, w, g, mean, rstd, gx, partials, rows, C, W);
     } else if (!with_row_threads<T>(C, [&](auto l, auto u) {
                    constexpr int L = decltype(l)::value, U = decltype(u)::value;
-                   if constexpr (L <= 64 ? U == 1 : L == 1024) {
+                   if constexpr (L <= 32 || L == 1024) {
                    constexpr int WG = rows_bwd_threads(L);
                    const dim3 wg(WG), grid((unsigned)(gw ? slices : std::min(cdiv64(rows, WG / L), WALKERS)));
                    auto launch = [&](auto params, auto narrow) {
