@@ -23,8 +23,8 @@ struct Param {
     __device__ __forceinline__ float operator[](int c) const { return sizeof(T) == 4 || f32 ? ((const float *)p)[c] : to_f32(((const T *)p)[c]); }
 };
 
-// Sum over the L threads that share a row: lanes of a wave, or a workgroup of L = 256 or 1024 through LDS (`place`: a slot of its own for
-// each sum between two barriers of the caller).
+// Sum over the L threads that share a row: lanes of a wave, or waves through LDS (`place`: slots of its own for each sum between two
+// barriers of the caller, one for each wave of the workgroup).
 template <int L>
 __device__ __forceinline__ float row_sum(float v, float *place)
 {
@@ -32,6 +32,7 @@ __device__ __forceinline__ float row_sum(float v, float *place)
     v = lanes_sum<64>(v);
     if ((threadIdx.x & 63) == 0) place[threadIdx.x >> 6] = v;
     __syncthreads();
+    place += (threadIdx.x >> 6) / (L / 64) * (L / 64);
     v = place[0];
 #pragma unroll
     for (int i = 1; i < L / 64; ++i) v += place[i];
@@ -58,6 +59,9 @@ __device__ __forceinline__ void store_columns(float *to, int c0, int C, const fl
 // ---- point-major ------------------------------------------------------------------------------------------------------------
 // L threads hold a row, U times 16 bytes each; a group of them takes R rows, which it asks for together.  NARROW: rows of fewer
 // channels than 16 bytes hold.
+// Memory bounds it where enough of it is asked for at once: the registers of R U = 3 to 4 pieces a thread, and few idle lanes.
+// 1M x 128 fp32: 176 us (1.03 GB, 5.9 TB/s).  x and y of 336 MB: bf16, 64 channels 66 us, 264 69 (by 64 lanes 86), 1100 67 (by 256 lanes
+// 123), 2100 68 (by 256 lanes 82), 4096 63; fp32, 64 channels 61, 2048 59, 4096 63.
 template <class T, int L, int U, int R, bool NARROW>
 __global__ __launch_bounds__(L > 256 ? L : 256) void norm_rows_kernel(const T *__restrict__ x, Param<T> w, Param<T> b, T *__restrict__ y,
                                                                       float *mean_out, float *rstd_out, int64_t rows, int C, float eps)
@@ -420,7 +424,7 @@ __global__ __launch_bounds__(rows_bwd_threads(L)) void norm_rows_bwd_kernel(cons
 // at least two.  A wave's vector operations decide beside the memory, 14 an element: nothing in a turn is chosen by a lane's place, what
 // is another lane's has weight 0 in the row's sums and is left out when the parameters' are stored.
 // 8188 x 5120 bf16: 46 us with the 4 us of the partial sums' sum (5.5 TB/s; adding x and grad_out 44), without the parameters' 42.
-// x, grad_out and grad_x of 504 MB: bf16, 264 channels 107 us (33 of 64 lanes), 512 98, 1000 100 (every other row off 16 bytes), 2048 97,
+// x, grad_out and grad_x of 504 MB: bf16, 264 channels 102 to 136 us (33 of 64 lanes), 512 98, 1000 100 (every other row off 16 bytes), 2048 97,
 // 8192 101; fp32, 132 channels 96, 1024 95, 4096 97.
 template <class T, bool PARAMS, bool GRAD_X, int D>
 __global__ __launch_bounds__(1024) void norm_wide_rows_bwd_kernel(const T *__restrict__ x, Param<T> w, const T *__restrict__ g,
@@ -790,7 +794,8 @@ __global__ __launch_bounds__(1024) void norm_params_sum_kernel(const float *__re
 
 // ---- launches -----------------------------------------------------------------------------------------------------------------
 
-// The row kernels' threads and 16-byte pieces: the smallest that hold C.  f(L, U); false: none.
+// The row kernels' threads and 16-byte pieces: the smallest that hold C, in steps of at most a half, up to what one wave holds.  f(L, U);
+// false: none.
 template <class T, class F>
 static bool with_row_threads(int C, F f)
 {
@@ -801,9 +806,13 @@ static bool with_row_threads(int C, F f)
     FLEX_ROW_THREADS(8, 1)
     FLEX_ROW_THREADS(16, 1)
     FLEX_ROW_THREADS(32, 1)
+    FLEX_ROW_THREADS(16, 3)
     FLEX_ROW_THREADS(64, 1)
+    FLEX_ROW_THREADS(32, 3)
     FLEX_ROW_THREADS(64, 2)
-    FLEX_ROW_THREADS(256, 1)
+    FLEX_ROW_THREADS(64, 3)
+    FLEX_ROW_THREADS(64, 4)
+    FLEX_ROW_THREADS(128, 3)
     FLEX_ROW_THREADS(256, 2)
     FLEX_ROW_THREADS(256, 3)
     FLEX_ROW_THREADS(256, 4)
@@ -831,7 +840,7 @@ static bool wide_rows(int C, int lane) { return C > 32 * lane && C <= 1024 * lan
 static int wide_waves(int C, int lane) { return (C + 64 * lane - 1) / (64 * lane); }
 
 // Rows that a group of the forward pass takes together
-constexpr int rows_together(int L, int U) { return L <= 64 && U == 1 ? 4 : L == 64 ? 2 : 1; }
+constexpr int rows_together(int L, int U) { return L > 64 || U == 4 ? 1 : U == 1 ? 4 : 2; }
 
 // Threads of a launch that has some for every position, at most
 static int64_t norm_threads(int B, int N, int C, int dtype, bool bcn)
@@ -925,7 +934,7 @@ static hipError_t launch_norm_bwd(const T *x, const void *weight, const T *g, co
         else hipLaunchKernelGGL((norm_wide_rows_bwd_kernel<T, true, false, 3>), grid, wg, 0, s, x, w, g, mean, rstd, gx, partials, rows, C, W);
     } else if (!with_row_threads<T>(C, [&](auto l, auto u) {
                    constexpr int L = decltype(l)::value, U = decltype(u)::value;
-                   if constexpr (L <= 32 || L == 1024) {
+                   if constexpr (U == 1 || L == 1024) {
                    constexpr int WG = rows_bwd_threads(L);
                    const dim3 wg(WG), grid((unsigned)(gw ? slices : std::min(cdiv64(rows, WG / L), WALKERS)));
                    auto launch = [&](auto params, auto narrow) {

@@ -12,7 +12,8 @@ pytestmark = pytest.mark.gpu
 
 SHAPES = [(1, 1, 1), (1, 1, 4096), (2, 3, 2), (1, 65, 3), (3, 41, 9), (1, 1000, 13), (2, 129, 16), (1, 64, 63), (1, 300, 64), (2, 70, 65),
           (1, 513, 100), (1, 33, 128), (1, 5, 255), (2, 17, 257), (1, 40, 513), (1, 21, 1000), (1, 9, 2049), (2, 5, 5120), (1, 3, 8191),
-          (1, 7, 16000), (1, 2, 33000), (1, 4100, 48), (1, 20011, 4)]
+          (1, 7, 16000), (1, 2, 33000), (1, 4100, 48), (1, 20011, 4), (1, 19, 130), (1, 70, 300), (3, 23, 385), (3, 11, 700), (1, 9, 1400),
+          (2, 7, 2500), (1, 6001, 1030), (1, 1301, 4500)]
 
 
 def make(seed, B, N, C, dtype, shift=0.5):
