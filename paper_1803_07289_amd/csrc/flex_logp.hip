@@ -58,10 +58,27 @@ __device__ __forceinline__ void store_sums(const LogpArgs &a, int64_t row, float
     a.entropy[row] = k.s == 0.f ? 0.f : log_s - k.u / k.s;
     a.lse[row] = k.m + log_s;
 }
+struct Alternative {
+    float logp;
+    int c;
+    __device__ __forceinline__ Alternative() {}
+    __device__ __forceinline__ Alternative(float v, int c, const Sums &k, float log_s)
+        : logp(v == -INFINITY ? -INFINITY : v - k.m - log_s), c(v == -INFINITY ? -1 : c) {}
+};
 __device__ __forceinline__ void store_top(const LogpArgs &a, int64_t at, float v, int c, const Sums &k, float log_s)
 {
-    a.top_logp[at] = v == -INFINITY ? -INFINITY : v - k.m - log_s;
-    a.top_class[at] = v == -INFINITY ? -1 : c;
+    const Alternative t(v, c, k, log_s);
+    a.top_logp[at] = t.logp;
+    a.top_class[at] = t.c;
+}
+// n of them behind one another
+template <int n>
+__device__ __forceinline__ void store_tops(const LogpArgs &a, int64_t at, const Alternative (&t)[4])
+{
+#pragma unroll
+    for (int q = 0; q < n; ++q) a.top_logp[at + q] = t[q].logp;
+#pragma unroll
+    for (int q = 0; q < n; ++q) a.top_class[at + q] = t[q].c;
 }
 __device__ __forceinline__ bool ignored(const LogpArgs &a, int t) { return a.target && (t < 0 || t >= a.C); }
 
@@ -516,6 +533,48 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void logp_lanes_kernel(const
         if (skip) a.logp[row] = a.entropy[row] = a.lse[row] = 0.f;
         else store_sums(a, row, a.target ? to_f32(at[t * step]) : 0.f, k, log_s);
     }
+    if (W == 1) {
+        // the first of those that are the maximum goes at once: three vector operations an element
+        const auto next = [&]() {
+            best = -INFINITY;
+#pragma unroll
+            for (int r = 0; r < R; ++r) best = fmaxf(best, v[r]);
+            bool found = false;
+            int c = NO_CLASS;
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                const bool hit = v[r] == best && !found;
+                found |= hit;
+                c = hit ? r : c;
+                v[r] = hit ? -INFINITY : v[r];
+            }
+            return Alternative(skip ? -INFINITY : best, c, k, log_s);
+        };
+        if (!ROWS) {
+            for (int i = 0; i < a.top; ++i) {
+                const Alternative t = next();
+                const int64_t to = (b * a.top + i) * a.N + n;
+                if (mine) a.top_logp[to] = t.logp;
+                if (mine) a.top_class[to] = t.c;
+            }
+            return;
+        }
+        // (four at a time: a row's lie behind one another)
+        for (int i = 0; i < a.top; i += 4) {
+            Alternative t[4];
+            const int many = min(4, a.top - i);
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+                if (q < many) t[q] = next();
+            if (!mine) continue;
+            const int64_t to = row * a.top + i;
+            if (many == 4) store_tops<4>(a, to, t);
+            else if (many == 3) store_tops<3>(a, to, t);
+            else if (many == 2) store_tops<2>(a, to, t);
+            else store_tops<1>(a, to, t);
+        }
+        return;
+    }
     float last_best = INFINITY;
     int last_class = -1;
     for (int i = 0; i < a.top; ++i) {
@@ -531,18 +590,16 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void logp_lanes_kernel(const
                 if (y > best && (y < last_best || (y == last_best && r > last_class))) { best = y; c = r; }
             }
         }
-        if (W > 1) {
-            s_best[wave][lane] = best;
-            s_class[wave][lane] = c;
-            __syncthreads();
-            best = s_best[0][lane];
-            c = s_class[0][lane];
+        s_best[wave][lane] = best;
+        s_class[wave][lane] = c;
+        __syncthreads();
+        best = s_best[0][lane];
+        c = s_class[0][lane];
 #pragma unroll
-            for (int w = 1; w < W; ++w)
-                if (s_best[w][lane] > best) { best = s_best[w][lane]; c = s_class[w][lane]; }
-            __syncthreads();
-        }
-        if (wave == 0 && mine) store_top(a, ROWS ? row * a.top + i : (b * a.top + i) * a.N + n, skip ? -INFINITY : best, c, k, log_s);
+        for (int w = 1; w < W; ++w)
+            if (s_best[w][lane] > best) { best = s_best[w][lane]; c = s_class[w][lane]; }
+        __syncthreads();
+        if (wave == 0 && mine) store_top(a, (b * a.top + i) * a.N + n, skip ? -INFINITY : best, c, k, log_s);
         last_best = best;
         last_class = c;
         if (R)
