@@ -454,9 +454,6 @@ __global__ __launch_bounds__(64) void logp_join_kernel(const T *__restrict__ x, 
 }
 
 // ---- channel-major, and point-major rows of few classes ----------------------------------------------------------------------
-// A lane to a position, W waves of a workgroup share the classes: R of them a wave in registers, or (R = 0) any number, read again
-// for each alternative.  What the waves find meets in LDS.
-// ROWS: point-major; the lanes of a wave read their rows 16 bytes at a time, which fills whole lines over a few loads.
 // A row of C <= R elements to a lane; what lies behind it is left as it is.
 template <class T, int R>
 __device__ __forceinline__ void load_few(const T *row, int C, float (&v)[R])
@@ -476,6 +473,11 @@ __device__ __forceinline__ void load_few(const T *row, int C, float (&v)[R])
     }
 }
 
+// A lane to a position, W waves of a workgroup share the classes: R of them a wave in registers, or (R = 0) any number, read again
+// for each alternative.  What the waves find meets in LDS.
+// ROWS: point-major; the lanes of a wave read their rows 16 bytes at a time, which fills whole lines over a few loads.
+// 1M x 13 fp32 with 3 alternatives, point-major: 18.9 us, 92 MB (without alternatives 13.6, 68 MB); channel-major 21 (13.9).  A wave's
+// stores decide beside the memory: those of a row's alternatives, 4 bytes at a time, made it 21.6.
 template <class T, int W, int R, bool ROWS>
 __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void logp_lanes_kernel(const T *__restrict__ x, LogpArgs a)
 {
@@ -744,12 +746,13 @@ static size_t parts_sums_bytes(int64_t rows, int parts) { return align256((size_
 template <class T>
 static hipError_t launch_logp_rows(const T *x, const LogpArgs &a, int dtype, void *ws, hipStream_t s)
 {
-    // A lane to a row up to 24 classes: us, four or eight lanes to a row and one, 2M rows, top 3: fp32, 13 classes 48 and 46, 17 classes
-    // 92 and 53, 24 classes 95 and 64, 32 classes 97 and 109; bf16, 17 classes 59 and 40, 24 classes 61 and 45.
-    if (a.C <= 24) {
+    // A lane to a row up to 32 classes: us, four or eight lanes to a row and one, 2M rows, top 3: fp32, 13 classes 59 and 40, 17 classes
+    // 96 and 49, 24 classes 95 and 64, 32 classes 94 and 90; bf16, 13 classes 67 and 38, 24 classes 61 and 43, 32 classes 58 and 53.
+    if (a.C <= 32) {
         const dim3 grid((unsigned)cdiv64(a.rows, 256));
         if (a.C <= 16) hipLaunchKernelGGL((logp_lanes_kernel<T, 1, 16, true>), grid, dim3(256), 0, s, x, a);
-        else hipLaunchKernelGGL((logp_lanes_kernel<T, 1, 24, true>), grid, dim3(256), 0, s, x, a);
+        else if (a.C <= 24) hipLaunchKernelGGL((logp_lanes_kernel<T, 1, 24, true>), grid, dim3(256), 0, s, x, a);
+        else hipLaunchKernelGGL((logp_lanes_kernel<T, 1, 32, true>), grid, dim3(256), 0, s, x, a);
         return hipGetLastError();
     }
     if (a.C <= row_columns_max(dtype))
