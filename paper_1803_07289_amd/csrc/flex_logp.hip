@@ -82,85 +82,7 @@ __device__ __forceinline__ void store_tops(const LogpArgs &a, int64_t at, const 
 }
 __device__ __forceinline__ bool ignored(const LogpArgs &a, int t) { return a.target && (t < 0 || t >= a.C); }
 
-// ---- point-major, rows of up to 64 lanes' elements ------------------------------------------------------------------------
-// L lanes hold a row, U times 16 bytes each.  The best score is the maximum over the lanes, its class the smallest among those that
-// hold it; it is then taken out, and so on for each alternative: 2 log2 L steps and three operations an element each.
-template <class T, int L, int U>
-__global__ __launch_bounds__(256) void logp_rows_kernel(const T *__restrict__ x, LogpArgs a)
-{
-    constexpr int N = LANE_ELEMENTS<T>;
-    const int sub = threadIdx.x % L;
-    const int64_t row = (int64_t)blockIdx.x * (256 / L) + threadIdx.x / L;
-    const bool mine = row < a.rows;
-    const int t = mine && a.target ? a.target[row] : 0;
-    const bool skip = !mine || ignored(a, t);
-    const T *at = x + row * a.stride;
-    float v[U][N];
-    int from[U];
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-        const int c0 = (u * L + sub) * N;
-        from[u] = Chunk<T>::from(c0, a.C);
-#pragma unroll
-        for (int j = 0; j < N; ++j) v[u][j] = -INFINITY;
-        if (!skip) Chunk<T>::load(at + from[u], v[u]);
-    }
-#pragma unroll
-    for (int u = 0; u < U; ++u) Chunk<T>::mask(v[u], (u * L + sub) * N, a.C, -INFINITY);
-    const float target_score = !skip && sub == 0 && a.target ? to_f32(at[t]) : 0.f;
-    float best = -INFINITY;
-#pragma unroll
-    for (int u = 0; u < U; ++u)
-#pragma unroll
-        for (int j = 0; j < N; ++j) best = fmaxf(best, v[u][j]);
-    best = lanes_max<L>(best);
-    Sums k{centre(best), 0.f, 0.f};
-#pragma unroll
-    for (int u = 0; u < U; ++u)
-#pragma unroll
-        for (int j = 0; j < N; ++j) add_score(k, v[u][j], k.m);
-    k.s = lanes_sum<L>(k.s);
-    k.u = lanes_sum<L>(k.u);
-    const float log_s = logf(k.s);
-    if (mine && sub == 0) {
-        if (skip) {
-            a.logp[row] = a.entropy[row] = a.lse[row] = 0.f;
-        } else
-            store_sums(a, row, target_score, k, log_s);
-    }
-    for (int i = 0; i < a.top; ++i) {
-        int c = NO_CLASS;
-#pragma unroll
-        for (int u = U - 1; u >= 0; --u)
-#pragma unroll
-            for (int j = N - 1; j >= 0; --j)
-                if (v[u][j] == best) c = from[u] + j;
-        c = lanes_min<L>(c);
-        if (mine && sub == i % L) store_top(a, row * a.top + i, best, c, k, log_s);
-        if (i + 1 == a.top) break;
-        best = -INFINITY;
-#pragma unroll
-        for (int u = 0; u < U; ++u)
-#pragma unroll
-            for (int j = 0; j < N; ++j) {
-                if (from[u] + j == c) v[u][j] = -INFINITY;
-                best = fmaxf(best, v[u][j]);
-            }
-        best = lanes_max<L>(best);
-    }
-}
-
-// ---- point-major, longer rows ---------------------------------------------------------------------------------------------
-// A workgroup runs along a part of a row, 16 KB at a time, the next 16 KB on their way meanwhile.  A lane's sums are about its own
-// maximum so far and meet at the end.  What an element costs decides beside the memory (bf16: 2 bytes in the time of some 11 vector
-// operations): exp counts four, the product and difference in front of it are one fused operation, the maximum takes two elements a
-// step.
-// Alternatives: the `top`-th largest of the 64 maxima that four lanes each have met so far is reached by `top` scores of the part, so
-// only what reaches it can be among the best; that goes to the wave's list in LDS.  The bound is found after the first span and
-// renewed when as many again have passed, from whatever maxima the other waves have left by then: each is a score of the part,
-// and an older one is a lower bound too.  A list that fills up (rows of equal scores, ascending rows) is cut to the best `top`;
-// scores of later spans then have to exceed the last of them.  The lists meet in one, cut by the largest bound of the four waves,
-// and are ranked there.  Parts of one row meet in logp_join_kernel.
+// ---- the best of many ------------------------------------------------------------------------------------------------------
 
 // the bits of a float, ordered like the floats (of the two zeros the positive one: they are equal)
 __device__ __forceinline__ uint32_t order_key(float v)
@@ -237,6 +159,139 @@ __device__ __forceinline__ void lds_in_order()
     __builtin_amdgcn_wave_barrier();
 }
 
+// ---- point-major, rows that a wave holds ----------------------------------------------------------------------------------
+// L lanes hold a row, U times 16 bytes each.  A wave's operations decide beside the memory (bf16: 2 bytes in the time of some 10 of
+// them), so that lanes hold many elements, and few of them nothing: the steps of a reduction are shared by more.
+// The best score is the maximum over the lanes, its class the smallest among those that hold it; it is then taken out of its 16 bytes,
+// the only ones that are looked at, and so on for each alternative: some 70 operations.  Where a row has the wave to itself and more
+// than four are asked for, what reaches the `top`-th largest of the lanes' maxima is listed and ranked, in the time of six.
+// us for 336 MB of scores, 0, 1 and 20 alternatives: bf16, 64 classes 82, 88 and 527, 256 classes 89, 95 and 437, 300 classes 91, 98 and 424,
+// 1500 classes 79, 85 and 132 (by the longer rows' workgroups 291, 467 and 550), 4096 classes 104, 110 and 176 (118, 173 and 209);
+// fp32, 64 classes 65, 68 and 312, 600 classes 67, 74 and 122 (241, 413 and 473), 2048 classes 57, 58 and 88 (79, 131 and 151).
+constexpr int ROW_LIST = 96;
+template <class T, int L, int U>
+__global__ __launch_bounds__(256) void logp_rows_kernel(const T *__restrict__ x, LogpArgs a)
+{
+    constexpr int N = LANE_ELEMENTS<T>;
+    __shared__ Candidate s_list[L == 64 ? 4 : 1][ROW_LIST];
+    const int sub = threadIdx.x % L;
+    const int64_t row = (int64_t)blockIdx.x * (256 / L) + threadIdx.x / L;
+    const bool mine = row < a.rows;
+    const int t = mine && a.target ? a.target[row] : 0;
+    const bool skip = !mine || ignored(a, t);
+    const T *at = x + row * a.stride;
+    float v[U][N], most[U];
+    int from[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        from[u] = Chunk<T>::from((u * L + sub) * N, a.C);
+#pragma unroll
+        for (int j = 0; j < N; ++j) v[u][j] = -INFINITY;
+        if (!skip) Chunk<T>::load(at + from[u], v[u]);
+    }
+    const float target_score = !skip && sub == 0 && a.target ? to_f32(at[t]) : 0.f;
+    float best = -INFINITY;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        Chunk<T>::mask(v[u], (u * L + sub) * N, a.C, -INFINITY);
+        most[u] = v[u][0];
+#pragma unroll
+        for (int j = 1; j < N; ++j) most[u] = fmaxf(most[u], v[u][j]);
+        best = fmaxf(best, most[u]);
+    }
+    const float own_best = best;
+    best = lanes_max<L>(best);
+    Sums k{centre(best), 0.f, 0.f};
+    if (!__any(fabsf(k.m) > HUGE_SCORE)) {
+        const float shift = k.m * LOG2E;
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int j = 0; j < N; ++j) {
+                const float z = __builtin_fmaf(v[u][j], LOG2E, -shift), e = __builtin_amdgcn_exp2f(z);
+                k.s += e;
+                k.u = __builtin_fmaf(e, fmaxf(z, MASKED), k.u);
+            }
+        k.u *= LN2;
+    } else {
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int j = 0; j < N; ++j) add_score(k, v[u][j], k.m);
+    }
+    k.s = lanes_sum<L>(k.s);
+    k.u = lanes_sum<L>(k.u);
+    const float log_s = logf(k.s);
+    if (mine && sub == 0) {
+        if (skip) {
+            a.logp[row] = a.entropy[row] = a.lse[row] = 0.f;
+        } else
+            store_sums(a, row, target_score, k, log_s);
+    }
+    if (a.top == 0) return;
+    if (L == 64 && a.top > 4) {
+        const float least = reached_by(own_best, a.top);
+        int count = least == -INFINITY ? ROW_LIST + 1 : 0;
+        Candidate *const list = s_list[threadIdx.x >> 6];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (!__any(most[u] >= least)) continue;
+#pragma unroll
+            for (int j = 0; j < N; ++j) {
+                const uint64_t takers = __ballot(v[u][j] >= least);
+                if (!takers) continue;
+                const int place = count + (int)__builtin_amdgcn_mbcnt_hi((unsigned)(takers >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)takers, 0));
+                if (v[u][j] >= least && place < ROW_LIST) list[place] = candidate(v[u][j], from[u] + j);
+                count += __popcll(takers);
+            }
+        }
+        if (count <= ROW_LIST) {        // (otherwise one after another, as below)
+            lds_in_order();
+            each_ranked(list, count, sub, 64, [&](int rank, Candidate e) {
+                if (rank < a.top) store_top(a, row * a.top + rank, score_of(e), class_of(e), k, log_s);
+            });
+            return;
+        }
+    }
+    for (int i = 0; i < a.top; ++i) {
+        int c = NO_CLASS;
+#pragma unroll
+        for (int u = U - 1; u >= 0; --u)
+            if (most[u] == best)
+#pragma unroll
+                for (int j = N - 1; j >= 0; --j)
+                    if (v[u][j] == best) c = from[u] + j;
+        c = lanes_min<L>(c);
+        if (mine && sub == i % L) store_top(a, row * a.top + i, best, c, k, log_s);
+        if (i + 1 == a.top) break;
+        float next = -INFINITY;
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (most[u] == best) {
+                most[u] = -INFINITY;
+#pragma unroll
+                for (int j = 0; j < N; ++j) {
+                    if (from[u] + j == c) v[u][j] = -INFINITY;
+                    most[u] = fmaxf(most[u], v[u][j]);
+                }
+            }
+            next = fmaxf(next, most[u]);
+        }
+        best = lanes_max<L>(next);
+    }
+}
+
+// ---- point-major, longer rows ---------------------------------------------------------------------------------------------
+// A workgroup runs along a part of a row, 16 KB at a time, the next 16 KB on their way meanwhile.  A lane's sums are about its own
+// maximum so far and meet at the end.  What an element costs decides beside the memory (bf16: 2 bytes in the time of some 11 vector
+// operations): exp counts four, the product and difference in front of it are one fused operation, the maximum takes two elements a
+// step.
+// Alternatives: the `top`-th largest of the 64 maxima that four lanes each have met so far is reached by `top` scores of the part, so
+// only what reaches it can be among the best; that goes to the wave's list in LDS.  The bound is found after the first span and
+// renewed when as many again have passed, from whatever maxima the other waves have left by then: each is a score of the part,
+// and an older one is a lower bound too.  A list that fills up (rows of equal scores, ascending rows) is cut to the best `top`;
+// scores of later spans then have to exceed the last of them.  The lists meet in one, cut by the largest bound of the four waves,
+// and are ranked there.  Parts of one row meet in logp_join_kernel.
 template <class T>
 __global__ __launch_bounds__(256) void logp_part_kernel(const T *__restrict__ x, LogpArgs a, LogpParts p)
 {
@@ -640,7 +695,9 @@ struct LogpBwdRow {
     }
 };
 
-// Point-major: L lanes to a row, U times 16 bytes each, `chunks` workgroups behind one another along long rows (L = 256).
+// Point-major: L lanes to a row, U times 16 bytes each, `chunks` workgroups behind one another along long rows (L = 256).  Bound by memory
+// where rows fill their lanes: 336 MB of scores and as much of gradients, bf16, 64 classes 126 us (5.3 TB/s), 100 classes 210, 600 117, 131072
+// 112 (6.0 TB/s); fp32, 40 classes 164, 512 114, 131072 118.
 template <class T, int L, int U>
 __global__ __launch_bounds__(256) void logp_bwd_rows_kernel(const T *x, T *gx, LogpBwdArgs a, int chunks)
 {
@@ -715,19 +772,57 @@ __global__ __launch_bounds__(256) void logp_bwd_cols_kernel(const T *x, T *gx, L
 
 // ---- launches -------------------------------------------------------------------------------------------------------------
 
-// Columns that a row kernel of (L, U) holds; the smallest that holds C is taken.
+// f(L, U) with the first of these lanes and 16-byte pieces that hold C.
+#define FLEX_ROW_LANES(L, U) \
+    if (C <= L * U * LANE_ELEMENTS<T>) return f(std::integral_constant<int, L>{}, std::integral_constant<int, U>{});
 template <class T, class F>
 static hipError_t with_row_lanes(int C, F f)
 {
-    constexpr int N = LANE_ELEMENTS<T>;
-    if (C <= 4 * N) return f(std::integral_constant<int, 4>{}, std::integral_constant<int, 1>{});
-    if (C <= 8 * N) return f(std::integral_constant<int, 8>{}, std::integral_constant<int, 1>{});
-    if (C <= 16 * N) return f(std::integral_constant<int, 16>{}, std::integral_constant<int, 1>{});
-    if (C <= 32 * N) return f(std::integral_constant<int, 32>{}, std::integral_constant<int, 1>{});
-    if (C <= 64 * N) return f(std::integral_constant<int, 64>{}, std::integral_constant<int, 1>{});
-    return f(std::integral_constant<int, 64>{}, std::integral_constant<int, 2>{});
+    FLEX_ROW_LANES(4, 2)
+    FLEX_ROW_LANES(4, 3)
+    FLEX_ROW_LANES(4, 4)
+    FLEX_ROW_LANES(8, 3)
+    FLEX_ROW_LANES(8, 4)
+    FLEX_ROW_LANES(16, 3)
+    FLEX_ROW_LANES(16, 4)
+    FLEX_ROW_LANES(32, 3)
+    FLEX_ROW_LANES(32, 4)
+    FLEX_ROW_LANES(64, 3)
+    FLEX_ROW_LANES(64, 4)
+    FLEX_ROW_LANES(64, 6)
+    FLEX_ROW_LANES(64, 8)
+    return hipErrorInvalidValue;
 }
-static int row_columns_max(int dtype) { return 2048 / (int)dtype_bytes(dtype); }      // 64 lanes x 2 x 16 bytes
+// whole waves, for rows of more than 32 lanes' elements
+template <class T, class F>
+static hipError_t with_row_wave(int C, F f)
+{
+    FLEX_ROW_LANES(64, 1)
+    FLEX_ROW_LANES(64, 2)
+    return with_row_lanes<T>(C, f);
+}
+// the gradient: many lanes rather than many elements, whole lines at a time, but not half of them idle
+template <class T, class F>
+static hipError_t with_row_lanes_bwd(int C, F f)
+{
+    FLEX_ROW_LANES(4, 1)
+    FLEX_ROW_LANES(4, 2)
+    FLEX_ROW_LANES(4, 3)
+    FLEX_ROW_LANES(16, 1)
+    FLEX_ROW_LANES(8, 3)
+    FLEX_ROW_LANES(32, 1)
+    FLEX_ROW_LANES(16, 3)
+    FLEX_ROW_LANES(64, 1)
+    FLEX_ROW_LANES(32, 3)
+    FLEX_ROW_LANES(64, 2)
+    FLEX_ROW_LANES(64, 3)
+    FLEX_ROW_LANES(64, 4)
+    return hipErrorInvalidValue;
+}
+#undef FLEX_ROW_LANES
+// the most that a row kernel takes: 64 lanes x 8 x 16 bytes, the gradient's 64 x 4 x 16
+static int row_columns_max(int dtype) { return 8192 / (int)dtype_bytes(dtype); }
+static int row_columns_bwd_max(int dtype) { return 4096 / (int)dtype_bytes(dtype); }
 
 // How a long row is cut: into parts of whole spans, so many that there are eight workgroups to a compute unit, or that a part is one
 // span, at most PARTS_MAX.
@@ -755,12 +850,14 @@ static hipError_t launch_logp_rows(const T *x, const LogpArgs &a, int dtype, voi
         else hipLaunchKernelGGL((logp_lanes_kernel<T, 1, 32, true>), grid, dim3(256), 0, s, x, a);
         return hipGetLastError();
     }
-    if (a.C <= row_columns_max(dtype))
-        return with_row_lanes<T>(a.C, [&](auto l, auto u) {
+    if (a.C <= row_columns_max(dtype)) {
+        const auto launch = [&](auto l, auto u) {
             constexpr int L = decltype(l)::value, U = decltype(u)::value;
             hipLaunchKernelGGL((logp_rows_kernel<T, L, U>), dim3((unsigned)cdiv64(a.rows, 256 / L)), dim3(256), 0, s, x, a);
             return hipGetLastError();
-        });
+        };
+        return a.top > 4 && a.C > 32 * LANE_ELEMENTS<T> ? with_row_wave<T>(a.C, launch) : with_row_lanes<T>(a.C, launch);
+    }
     const PartPlan q = plan_parts(a.rows, a.C, dtype);
     const LogpParts p{(Sums *)ws, (Candidate *)((char *)ws + parts_sums_bytes(a.rows, q.parts)), q.parts, q.spans};
     hipLaunchKernelGGL(logp_part_kernel<T>, dim3((unsigned)(a.rows * q.parts)), dim3(256), 0, s, x, a, p);
@@ -798,8 +895,8 @@ static hipError_t launch_logp_bwd(const T *x, T *gx, const LogpBwdArgs &a, int B
         hipLaunchKernelGGL((logp_bwd_few_kernel<T, FEW>), dim3((unsigned)cdiv64(a.rows, 256)), dim3(256), 0, s, x, gx, a);
         return hipGetLastError();
     }
-    if (a.C <= row_columns_max(dtype))
-        return with_row_lanes<T>(a.C, [&](auto l, auto u) {
+    if (a.C <= row_columns_bwd_max(dtype))
+        return with_row_lanes_bwd<T>(a.C, [&](auto l, auto u) {
             constexpr int L = decltype(l)::value, U = decltype(u)::value;
             hipLaunchKernelGGL((logp_bwd_rows_kernel<T, L, U>), dim3((unsigned)cdiv64(a.rows, 256 / L)), dim3(256), 0, s, x, gx, a, 1);
             return hipGetLastError();
@@ -824,7 +921,7 @@ static int64_t logp_threads(int B, int N, int C, int dtype, int layout)
         return B * cdiv64(N, 256) * 256 * std::max(waves, cdiv64(C, BWD_CLASSES));
     }
     const int lane = 16 / (int)dtype_bytes(dtype);
-    int64_t threads = C <= row_columns_max(dtype) ? 4 : 256 * cdiv64(C, 256 * lane * 2);
+    int64_t threads = C <= row_columns_bwd_max(dtype) ? 4 : 256 * cdiv64(C, 256 * lane * 2);
     while (threads < 64 && threads * lane < C) threads *= 2;
     return (int64_t)B * N * threads;
 }

@@ -57,12 +57,12 @@ def test_sizes_that_one_launch_does_not_take_are_refused(L):
         assert L.flexnorm_bwd_workspace_bytes(1, most + 1, 1, 0, layout) == 0
         assert norm_fwd(L, N=most + 1, C=1, layout=layout) == 2
     assert L.flexnorm_bwd_workspace_bytes(1, most, 1, 0, 1) > 0 and L.flexnorm_bwd_workspace_bytes(1, most, 1, 0, 0) > 0
-    for rows, C in ((1 << 24, 1025), (1 << 22, 8193)):                        # 256 and 1024 threads to a row
+    for rows, C in ((1 << 24, 4000), (1 << 22, 8193)):                        # 256 and 1024 threads to a row
         assert norm_fwd(L, N=rows, C=C, dtype=1, pdtype=1) == 2 and norm_bwd(L, N=rows, C=C, dtype=1, pdtype=1, ws_bytes=1 << 40) == 2
         assert L.flexnorm_bwd_workspace_bytes(1, rows - 1, C, 1, 1) > 0
     assert norm_fwd(L, N=1 << 28, C=129, layout=0) == 2                        # 16 waves to 64 positions
-    assert L.flexlogp_fwd_workspace_bytes(1, (1 << 24) - 1, 1025, 0, 1, 1) > 0
-    assert logp_fwd(L, N=1 << 24, C=1025, row=1025, dtype=1) == 2 and logp_bwd(L, N=1 << 24, C=1025, row=1025, grow=1025, dtype=1) == 2
+    assert L.flexlogp_fwd_workspace_bytes(1, (1 << 23) - 1, 4097, 0, 1, 1) > 0
+    assert logp_fwd(L, N=1 << 23, C=4097, row=4097, dtype=1) == 2 and logp_bwd(L, N=1 << 23, C=4097, row=4097, grow=4097, dtype=1) == 2
     assert logp_fwd(L, N=1 << 28, C=129, layout=0, row=1 << 28) == 2 and logp_bwd(L, N=1 << 28, C=129, layout=0, row=1 << 28, grow=1 << 28) == 2
     tensors = (fx._AdamwTensor * 17)(*(fx._AdamwTensor(count=(1 << 31) - 1) for _ in range(17)))
     assert L.flexadamw_plan_bytes(tensors, 15) > 0 and L.flexadamw_plan_bytes(tensors, 17) == 0
