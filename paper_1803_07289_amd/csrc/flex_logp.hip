@@ -94,6 +94,21 @@ __device__ __forceinline__ float from_order_key(uint32_t k)
 {
     return __builtin_bit_cast(float, k ^ (k >> 31 ? 0x80000000u : 0xFFFFFFFFu));
 }
+// a 16-bit score in the upper half of a word, zeros of one sign, and back
+template <class T>
+__device__ __forceinline__ float upper_bits(float v)
+{
+    if constexpr (std::is_same<T, bf16>::value) return v;
+    const uint32_t b = __builtin_bit_cast(uint16_t, (_Float16)(v + 0.f));
+    return __builtin_bit_cast(float, b << 16);
+}
+template <class T>
+__device__ __forceinline__ float from_upper_bits(float v)
+{
+    const uint32_t b = __builtin_bit_cast(uint32_t, v);       // (of a negative number's key the lower half is ones)
+    if constexpr (std::is_same<T, bf16>::value) return __builtin_bit_cast(float, b & 0xFFFF0000u);
+    return (float)__builtin_bit_cast(_Float16, (uint16_t)(b >> 16));
+}
 // A candidate as one number, the better ones the larger: the score, then the class, lower ones first.
 typedef unsigned long long Candidate;
 __device__ __forceinline__ Candidate candidate(float v, int c) { return (Candidate)order_key(v) << 32 | (uint32_t)~c; }
@@ -163,11 +178,12 @@ __device__ __forceinline__ void lds_in_order()
 // L lanes hold a row, U times 16 bytes each.  A wave's operations decide beside the memory (bf16: 2 bytes in the time of some 10 of
 // them), so that lanes hold many elements, and few of them nothing: the steps of a reduction are shared by more.
 // The best score is the maximum over the lanes, its class the smallest among those that hold it; it is then taken out of its 16 bytes,
-// the only ones that are looked at, and so on for each alternative: some 70 operations.  Where a row has the wave to itself and more
+// the only ones that are looked at where a row has 32 lanes or more, and so on for each alternative.  Where a row has the wave to itself and more
 // than four are asked for, what reaches the `top`-th largest of the lanes' maxima is listed and ranked, in the time of six.
-// us for 336 MB of scores, 0, 1 and 20 alternatives: bf16, 64 classes 82, 88 and 527, 256 classes 89, 95 and 437, 300 classes 91, 98 and 424,
-// 1500 classes 79, 85 and 132 (by the longer rows' workgroups 291, 467 and 550), 4096 classes 104, 110 and 176 (118, 173 and 209);
-// fp32, 64 classes 65, 68 and 312, 600 classes 67, 74 and 122 (241, 413 and 473), 2048 classes 57, 58 and 88 (79, 131 and 151).
+// Scores of 16 bits go into one number with their classes, for which an element costs two operations instead of five.
+// us for 336 MB of scores, 0, 1 and 20 alternatives: bf16, 64 classes 81, 95 and 330, 256 classes 71, 84 and 286, 300 classes 83, 103 and 384,
+// 1500 classes 79, 94 and 132 (by the longer rows' workgroups 291, 467 and 550), 4096 classes 84, 103 and 135 (118, 173 and 209);
+// fp32, 64 classes 64, 67 and 242, 600 classes 66, 73 and 119 (241, 413 and 473), 2048 classes 56, 58 and 88 (79, 131 and 151).
 constexpr int ROW_LIST = 96;
 template <class T, int L, int U>
 __global__ __launch_bounds__(256) void logp_rows_kernel(const T *__restrict__ x, LogpArgs a)
@@ -253,21 +269,66 @@ __global__ __launch_bounds__(256) void logp_rows_kernel(const T *__restrict__ x,
             return;
         }
     }
+    // L alternatives, one to a lane, then L stores in one
+    float held = -INFINITY;
+    int held_class = -1;
+    const auto hold = [&](int i, float score, int c) {
+        const int place = i % L;
+        if (sub == place) {
+            held = score;
+            held_class = c;
+        }
+        if (mine && (place == L - 1 || i + 1 == a.top) && sub <= place) store_top(a, row * a.top + i - place + sub, held, held_class, k, log_s);
+    };
+    if constexpr (sizeof(T) == 2) {
+        // a score of 16 bits and its class in one number, the better ones the larger, no two alike; 0: none
+        uint32_t key[U][N], most_key[U], best_key = 0;
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            most_key[u] = 0;
+#pragma unroll
+            for (int j = 0; j < N; ++j) {
+                key[u][j] = v[u][j] > -INFINITY ? (order_key(upper_bits<T>(v[u][j])) & 0xFFFF0000u) | (uint32_t)(0xFFFF - from[u] - j) : 0u;
+                most_key[u] = max(most_key[u], key[u][j]);
+            }
+            best_key = max(best_key, most_key[u]);
+        }
+        for (int i = 0; i < a.top; ++i) {
+            best_key = lanes_reduce<L>(best_key, [](uint32_t a, uint32_t b) { return max(a, b); });
+            hold(i, best_key ? from_upper_bits<T>(from_order_key(best_key & 0xFFFF0000u)) : -INFINITY, 0xFFFF - (int)(best_key & 0xFFFFu));
+            if (i + 1 == a.top) break;
+            uint32_t next = 0;
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                if (L < 32 || most_key[u] == best_key) {        // (of few lanes some row's best is nearly always here)
+                    most_key[u] = 0;
+#pragma unroll
+                    for (int j = 0; j < N; ++j) {
+                        key[u][j] = key[u][j] == best_key ? 0u : key[u][j];
+                        most_key[u] = max(most_key[u], key[u][j]);
+                    }
+                }
+                next = max(next, most_key[u]);
+            }
+            best_key = next;
+        }
+        return;
+    }
     for (int i = 0; i < a.top; ++i) {
         int c = NO_CLASS;
 #pragma unroll
         for (int u = U - 1; u >= 0; --u)
-            if (most[u] == best)
+            if (L < 32 || most[u] == best)
 #pragma unroll
                 for (int j = N - 1; j >= 0; --j)
                     if (v[u][j] == best) c = from[u] + j;
         c = lanes_min<L>(c);
-        if (mine && sub == i % L) store_top(a, row * a.top + i, best, c, k, log_s);
+        hold(i, best, c);
         if (i + 1 == a.top) break;
         float next = -INFINITY;
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            if (most[u] == best) {
+            if (L < 32 || most[u] == best) {
                 most[u] = -INFINITY;
 #pragma unroll
                 for (int j = 0; j < N; ++j) {
@@ -793,11 +854,10 @@ static hipError_t with_row_lanes(int C, F f)
     FLEX_ROW_LANES(64, 8)
     return hipErrorInvalidValue;
 }
-// whole waves, for rows of more than 32 lanes' elements
+// whole waves, for rows of more than 64 lanes' elements
 template <class T, class F>
 static hipError_t with_row_wave(int C, F f)
 {
-    FLEX_ROW_LANES(64, 1)
     FLEX_ROW_LANES(64, 2)
     return with_row_lanes<T>(C, f);
 }
@@ -856,7 +916,9 @@ static hipError_t launch_logp_rows(const T *x, const LogpArgs &a, int dtype, voi
             hipLaunchKernelGGL((logp_rows_kernel<T, L, U>), dim3((unsigned)cdiv64(a.rows, 256 / L)), dim3(256), 0, s, x, a);
             return hipGetLastError();
         };
-        return a.top > 4 && a.C > 32 * LANE_ELEMENTS<T> ? with_row_wave<T>(a.C, launch) : with_row_lanes<T>(a.C, launch);
+        // a wave to a row against fewer lanes, us, 336 MB, 8 and 20 alternatives: bf16, 512 classes 196 and 239, 149 and 288, 1000 classes
+        // 126 and 155, 127 and 215; fp32, 256 classes 185 and 211, 120 and 243, 512 classes 105 and 126, 106 and 217
+        return a.top > 4 && a.C > 64 * LANE_ELEMENTS<T> ? with_row_wave<T>(a.C, launch) : with_row_lanes<T>(a.C, launch);
     }
     const PartPlan q = plan_parts(a.rows, a.C, dtype);
     const LogpParts p{(Sums *)ws, (Candidate *)((char *)ws + parts_sums_bytes(a.rows, q.parts)), q.parts, q.spans};

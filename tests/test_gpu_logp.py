@@ -14,7 +14,8 @@ pytestmark = pytest.mark.gpu
 SHAPES = [(1, 1, 1, 1), (1, 3, 2, 2), (2, 5, 3, 3), (1, 130, 7, 1), (1, 1000, 13, 3), (3, 67, 16, 5), (1, 200, 33, 32), (2, 31, 50, 8),
           (1, 64, 64, 4), (1, 33, 65, 20), (1, 77, 129, 3), (1, 20, 255, 32), (2, 9, 513, 8), (1, 12, 1000, 20), (1, 5, 4097, 32),
           (1, 3, 16385, 7), (1, 2, 50001, 20), (2, 1, 131072, 32), (1, 1, 200003, 0), (1, 1, 1 << 20, 5), (1, 300, 100, 0), (1, 90, 19, 6),
-          (2, 300, 24, 24), (1, 300, 27, 7), (1, 77, 32, 32)]
+          (2, 300, 24, 24), (1, 300, 27, 7), (1, 77, 32, 32), (2, 15, 120, 9), (1, 30, 190, 1), (1, 40, 300, 20), (1, 33, 700, 3),
+          (1, 21, 1500, 32), (1, 9, 2500, 8), (1, 7, 3900, 20)]
 
 
 def scores(seed, rows, C, dtype, spread=3.0):
