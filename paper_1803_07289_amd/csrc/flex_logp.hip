@@ -592,8 +592,9 @@ __device__ __forceinline__ void load_few(const T *row, int C, float (&v)[R])
 // A lane to a position, W waves of a workgroup share the classes: R of them a wave in registers, or (R = 0) any number, read again
 // for each alternative.  What the waves find meets in LDS.
 // ROWS: point-major; the lanes of a wave read their rows 16 bytes at a time, which fills whole lines over a few loads.
-// 1M x 13 fp32 with 3 alternatives, point-major: 18.9 us, 92 MB (without alternatives 13.6, 68 MB); channel-major 21 (13.9).  A wave's
-// stores decide beside the memory: those of a row's alternatives, 4 bytes at a time, made it 21.6.
+// 1M x 13 fp32 with 3 alternatives, point-major: 18.9 us, 92 MB (without alternatives 13.6, 68 MB); channel-major 20 (13.9).  A wave's
+// stores decide beside the memory: those of a row's alternatives, 4 bytes at a time, made it 21.6.  Channel-major, 168 MB of scores: fp32,
+// 16 classes 42 us, 64 39, 256 57, 400 67; bf16, 16 classes 55 (113 when each load was converted in a branch of its own), 64 57, 256 95, 400 101.
 template <class T, int W, int R, bool ROWS>
 __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void logp_lanes_kernel(const T *__restrict__ x, LogpArgs a)
 {
@@ -620,10 +621,15 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void logp_lanes_kernel(const
         if constexpr (ROWS) {
             // (an ignored row's scores lie in lines that its neighbours need: they are loaded beside the target, and not used)
             if (mine) load_few<T, R>(at, a.C, v);
-        } else
+        } else {
+            // (all loads before the first is converted, in no branch)
+            T raw[R ? R : 1];
+            const T *from = mine ? at : x;
 #pragma unroll
-            for (int i = 0; i < R; ++i)
-                if (!skip && first + i < last) v[i] = to_f32(at[(first + i) * step]);
+            for (int i = 0; i < R; ++i) raw[i] = from[min(first + i, a.C - 1) * step];
+#pragma unroll
+            for (int i = 0; i < R; ++i) v[i] = first + i < last ? to_f32(raw[i]) : -INFINITY;
+        }
 #pragma unroll
         for (int i = 0; i < R; ++i) best = fmaxf(best, v[i]);
         k.m = best;
@@ -632,9 +638,11 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void logp_lanes_kernel(const
         for (int i = 0; i < R; ++i)
             if (first + i / 4 * 4 < last) add_score(k, v[i], m);
     } else if (!skip) {
+#pragma unroll 8
         for (int c = first; c < last; ++c) best = fmaxf(best, to_f32(at[c * step]));
         k.m = best;
         const float m = centre(best);
+#pragma unroll 8
         for (int c = first; c < last; ++c) add_score(k, to_f32(at[c * step]), m);
     }
     if (W > 1) {
@@ -703,9 +711,12 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void logp_lanes_kernel(const
             for (int r = 0; r < R; ++r)
                 if (v[r] > best) { best = v[r]; c = first + r; }
         } else if (!skip) {
+#pragma unroll 8
             for (int r = first; r < last; ++r) {
                 const float y = to_f32(at[r * step]);
-                if (y > best && (y < last_best || (y == last_best && r > last_class))) { best = y; c = r; }
+                const bool better = y > best && (y < last_best || (y == last_best && r > last_class));
+                best = better ? y : best;
+                c = better ? r : c;
             }
         }
         s_best[wave][lane] = best;
@@ -808,7 +819,8 @@ __global__ __launch_bounds__(256) void logp_bwd_few_kernel(const T *x, T *gx, Lo
     }
 }
 
-// Channel-major: a lane to a position, a workgroup to 256 of them and 16 classes.
+// Channel-major: a lane to a position, a workgroup to 256 of them and 16 classes.  168 MB of scores and as much of gradients: fp32,
+// 16 classes 84 us, 64 78, 256 74; bf16, which a wave loads in half lines, 16 classes 110, 64 104, 256 94.
 constexpr int BWD_CLASSES = 16;
 template <class T>
 __global__ __launch_bounds__(256) void logp_bwd_cols_kernel(const T *x, T *gx, LogpBwdArgs a, unsigned tiles, unsigned parts)
@@ -823,8 +835,7 @@ __global__ __launch_bounds__(256) void logp_bwd_cols_kernel(const T *x, T *gx, L
     // (an ignored position's scores share their lines with its neighbours': nothing is saved by not reading them)
     T v[BWD_CLASSES];
 #pragma unroll
-    for (int i = 0; i < BWD_CLASSES; ++i)
-        if (i < many) v[i] = at[i * a.stride];
+    for (int i = 0; i < BWD_CLASSES; ++i) v[i] = at[min(i, many - 1) * a.stride];        // (in no branch: all before the first is converted)
     const LogpBwdRow f(a, b * a.N + n);
 #pragma unroll
     for (int i = 0; i < BWD_CLASSES; ++i)
@@ -933,10 +944,12 @@ static hipError_t launch_logp_cols(const T *x, const LogpArgs &a, int B, hipStre
 {
     const int64_t tiles = B * cdiv64(a.N, 64);
     const dim3 grid((unsigned)tiles), four((unsigned)cdiv64(tiles, 4));
-    if (a.C <= 16) hipLaunchKernelGGL((logp_lanes_kernel<T, 1, 16, false>), four, dim3(256), 0, s, x, a);
+    if (a.C <= 8) hipLaunchKernelGGL((logp_lanes_kernel<T, 1, 8, false>), four, dim3(256), 0, s, x, a);
+    else if (a.C <= 16) hipLaunchKernelGGL((logp_lanes_kernel<T, 1, 16, false>), four, dim3(256), 0, s, x, a);
     else if (a.C <= 32) hipLaunchKernelGGL((logp_lanes_kernel<T, 2, 16, false>), grid, dim3(128), 0, s, x, a);
     else if (a.C <= 64) hipLaunchKernelGGL((logp_lanes_kernel<T, 4, 16, false>), grid, dim3(256), 0, s, x, a);
     else if (a.C <= 128) hipLaunchKernelGGL((logp_lanes_kernel<T, 8, 16, false>), grid, dim3(512), 0, s, x, a);
+    else if (a.C <= 256) hipLaunchKernelGGL((logp_lanes_kernel<T, 16, 16, false>), grid, dim3(1024), 0, s, x, a);
     else hipLaunchKernelGGL((logp_lanes_kernel<T, 16, 0, false>), grid, dim3(1024), 0, s, x, a);
     return hipGetLastError();
 }

@@ -582,6 +582,8 @@ __global__ __launch_bounds__(256) void norm_long_rows_params_kernel(const T *__r
 
 // ---- channel-major ----------------------------------------------------------------------------------------------------------
 // A lane to a position, W waves of a workgroup share the channels: R of them a wave in registers, or (R = 0) any number, read again.
+// Bound by memory; 16-bit types, of which a wave loads half a line at a time, by the number of loads.  us, x of 168 MB, forward and backward: fp32,
+// 16 channels 82 and 134, 64 82 and 142, 200 80 and 119, 400 130 and 243; bf16, 16 channels 105 and 159, 64 114 and 176, 200 116 and 149.
 constexpr int COL_CHANNELS = 16;
 
 // sums over the waves of a workgroup, by position
@@ -612,12 +614,17 @@ __global__ __launch_bounds__(64 * W) void norm_cols_kernel(const T *__restrict__
     const int64_t base = cloud * C * (int64_t)N + min(n, N - 1);
     const float count = (float)C;
     float v[R ? R : 1], sum = 0.f, sq = 0.f;
+    T raw[R ? R : 1];        // (all loads before the first is converted, in no branch)
     if (R) {
 #pragma unroll
-        for (int i = 0; i < R; ++i) v[i] = first + i < last ? to_f32(x[base + (int64_t)(first + i) * N]) : 0.f;
+        for (int i = 0; i < R; ++i) raw[i] = x[base + (int64_t)min(first + i, C - 1) * N];
 #pragma unroll
-        for (int i = 0; i < R; ++i) sum += v[i];
+        for (int i = 0; i < R; ++i) {
+            v[i] = first + i < last ? to_f32(raw[i]) : 0.f;
+            sum += v[i];
+        }
     } else
+#pragma unroll 8
         for (int c = first; c < last; ++c) sum += to_f32(x[base + (int64_t)c * N]);
     const float ww = R && w.p && lane < last - first ? w[first + lane] : 1.f, bb = R && w.p && lane < last - first ? b[first + lane] : 0.f;
     const float mean = waves_sum<W>(sum, s_place[0]) / count;
@@ -628,6 +635,7 @@ __global__ __launch_bounds__(64 * W) void norm_cols_kernel(const T *__restrict__
             if (first + i < last) sq += d * d;
         }
     } else
+#pragma unroll 8
         for (int c = first; c < last; ++c) {
             const float d = to_f32(x[base + (int64_t)c * N]) - mean;
             sq += d * d;
@@ -642,6 +650,7 @@ __global__ __launch_bounds__(64 * W) void norm_cols_kernel(const T *__restrict__
             if (first + i < last) y[base + (int64_t)(first + i) * N] = (T)v[i];
     } else {
         if (!mine) return;
+#pragma unroll 8
         for (int c = first; c < last; ++c) {
             const float d = (to_f32(x[base + (int64_t)c * N]) - mean) * rstd;
             y[base + (int64_t)c * N] = (T)(w.p ? d * w[c] + b[c] : d);
@@ -677,15 +686,17 @@ __global__ __launch_bounds__(64 * W) void norm_cols_bwd_kernel(const T *__restri
         const bool mine = n < N;
         const int64_t base = (cloud * C + first) * (int64_t)N + min(n, N - 1), at = cloud * N + min(n, N - 1);
         float xh[R], gg[R], s1 = 0.f, s2 = 0.f;
+        T xr[R], gr[R];
 #pragma unroll
         for (int i = 0; i < R; ++i) {
-            xh[i] = i < many ? to_f32(x[base + (int64_t)i * N]) : 0.f;
-            gg[i] = i < many && mine ? to_f32(g[base + (int64_t)i * N]) : 0.f;
+            xr[i] = x[base + (int64_t)min(i, many - 1) * N];
+            gr[i] = g[base + (int64_t)min(i, many - 1) * N];
         }
         const float m = mean[at], r = rstd[at];
 #pragma unroll
         for (int i = 0; i < R; ++i) {
-            xh[i] = (xh[i] - m) * r;
+            xh[i] = (to_f32(xr[i]) - m) * r;
+            gg[i] = i < many && mine ? to_f32(gr[i]) : 0.f;
             const float h = gg[i] * lane_value(ww, i);
             s1 += h;
             s2 += h * xh[i];
@@ -730,6 +741,7 @@ __global__ __launch_bounds__(1024) void norm_many_cols_bwd_kernel(const T *__res
     const int64_t base = cloud * C * (int64_t)N + min(n, N - 1), at = cloud * N + min(n, N - 1);
     const float m = mean[at], r = rstd[at], count = (float)C;
     float s1 = 0.f, s2 = 0.f;
+#pragma unroll 8
     for (int c = first; c < last; ++c) {
         const float h = to_f32(g[base + (int64_t)c * N]) * (w.p ? w[c] : 1.f);
         s1 += h;
@@ -738,6 +750,7 @@ __global__ __launch_bounds__(1024) void norm_many_cols_bwd_kernel(const T *__res
     s1 = waves_sum<W>(s1, s_place[0]) / count;
     s2 = waves_sum<W>(s2, s_place[1]) / count;
     if (n >= N) return;
+#pragma unroll 8
     for (int c = first; c < last; ++c) {
         const float h = to_f32(g[base + (int64_t)c * N]) * (w.p ? w[c] : 1.f);
         gx[base + (int64_t)c * N] = (T)((h - s1 - (to_f32(x[base + (int64_t)c * N]) - m) * r * s2) * r);
