@@ -205,6 +205,10 @@ __device__ __forceinline__ void store8(T *p, const float (&x)[8], int64_t at, in
             if (at + i < count) p[at + i] = (T)x[i];
 }
 
+// A workgroup to 2048 elements of a tensor, eight to a thread, which makes every access 16 or 8 bytes a lane and a scale's 32 elements
+// four lanes.  Memory bounds it: 5.4 TB/s with states in 32 bits and a copy (28 bytes an element, 191M elements: 997 us; at the rate of a copy 869),
+// 5.7 with states in 8 (10.1 bytes, 428M elements in bf16: 765 us, 704), where the vector unit has some 60 operations an element to hide.  Larger
+// pieces, two pieces a workgroup and accesses past the caches measured the same or worse.
 template <class P, class G, int BITS>
 __global__ __launch_bounds__(256) void adamw_step_kernel(AdamwPlan plan, int copy_dtype)
 {

@@ -353,6 +353,9 @@ __global__ __launch_bounds__(256) void logp_rows_kernel(const T *__restrict__ x,
 // and an older one is a lower bound too.  A list that fills up (rows of equal scores, ascending rows) is cut to the best `top`;
 // scores of later spans then have to exceed the last of them.  The lists meet in one, cut by the largest bound of the four waves,
 // and are ranked there.  Parts of one row meet in logp_join_kernel.
+// 2046 x 129280 bf16, a tenth ignored, 8 alternatives: 89 us (476 MB, 5.3 TB/s).  One row of 131072 bf16, 20 alternatives: 6 us in 16 parts
+// and 4.5 to join them.  336 MB of scores, 0, 1 and 20 alternatives: bf16, 5000 classes 95, 143 and 176 us (a span is 8192), 131072 classes
+// 55, 59 and 72; fp32, 4096 classes 49, 70 and 83, 131072 classes 55, 59 and 71.
 template <class T>
 __global__ __launch_bounds__(256) void logp_part_kernel(const T *__restrict__ x, LogpArgs a, LogpParts p)
 {

@@ -424,8 +424,8 @@ __global__ __launch_bounds__(rows_bwd_threads(L)) void norm_rows_bwd_kernel(cons
 // at least two.  A wave's vector operations decide beside the memory, 14 an element: nothing in a turn is chosen by a lane's place, what
 // is another lane's has weight 0 in the row's sums and is left out when the parameters' are stored.
 // 8188 x 5120 bf16: 46 us with the 4 us of the partial sums' sum (5.5 TB/s; adding x and grad_out 44), without the parameters' 42.
-// x, grad_out and grad_x of 504 MB: bf16, 264 channels 102 to 136 us (33 of 64 lanes), 512 98, 1000 100 (every other row off 16 bytes), 2048 97,
-// 8192 101; fp32, 132 channels 96, 1024 95, 4096 97.
+// x, grad_out and grad_x of 504 MB: bf16, 264 channels 102 to 136 us (33 of 64 lanes), 512 98, 1000 100, 2048
+// 97, 8192 101; fp32, 132 channels 96, 1024 95, 4096 97.
 template <class T, bool PARAMS, bool GRAD_X, int D>
 __global__ __launch_bounds__(1024) void norm_wide_rows_bwd_kernel(const T *__restrict__ x, Param<T> w, const T *__restrict__ g,
                                                                   const float *__restrict__ mean, const float *__restrict__ rstd,
@@ -871,7 +871,8 @@ static int64_t norm_threads(int B, int N, int C, int dtype, bool bcn)
 }
 constexpr int64_t WALKERS = 1 << 20;        // workgroups, at most, of those backward kernels that walk over the positions
 
-// Partial sums of grad_w and grad_b: the workgroups that walk over the positions, four turns at least to each.
+// Partial sums of grad_w and grad_b: the workgroups that walk over the positions, four turns at least to each where there are more than 64
+// (us, four turns always and this: fp32, 9 x 11650 28.7 and 17.4; bf16, 40 x 1000 9.4 and 7.4, 1000 x 768 10.9 and 8.9).
 static int norm_slices(int B, int N, int C, int dtype, bool bcn)
 {
     const int64_t rows = (int64_t)B * N, cus = device_cu_count();
@@ -885,7 +886,7 @@ static int norm_slices(int B, int N, int C, int dtype, bool bcn)
     int groups = wide_rows(C, lane) ? 16 / wide_waves(C, lane) : 1;
     for (const int L : {32, 16, 8, 4})
         if (C <= L * lane) groups = 256 / L;
-    return (int)std::max<int64_t>(1, std::min<int64_t>(cdiv64(rows, 4 * groups), C <= 32 * lane ? 4 * cus : cus));
+    return (int)std::min({cdiv64(rows, groups), std::max<int64_t>(64, cdiv64(rows, 4 * groups)), C <= 32 * lane ? 4 * cus : cus});
 }
 
 template <class T>
@@ -930,38 +931,50 @@ static hipError_t launch_norm_bwd(const T *x, const void *weight, const T *g, co
         const unsigned tiles = (unsigned)(N + 63) / 64, total = (unsigned)B * tiles;
         with_col_waves(C, [&](auto waves) {
             constexpr int W = decltype(waves)::value;
-            if (gw) hipLaunchKernelGGL((norm_cols_bwd_kernel<T, W, true>), dim3((unsigned)slices), dim3(64 * W), 0, s, x, w, g, mean, rstd, gx, partials, N, C, tiles, total);
-            else hipLaunchKernelGGL((norm_cols_bwd_kernel<T, W, false>), dim3((unsigned)std::min<int64_t>(total, WALKERS)), dim3(64 * W), 0, s, x, w, g, mean, rstd, gx, partials, N, C, tiles, total);
+            auto launch = [&](auto params, int64_t workgroups) {
+                hipLaunchKernelGGL((norm_cols_bwd_kernel<T, W, decltype(params)::value>), dim3((unsigned)workgroups), dim3(64 * W), 0, s, x, w, g,
+                                   mean, rstd, gx, partials, N, C, tiles, total);
+            };
+            if (gw) launch(std::true_type{}, slices);
+            else launch(std::false_type{}, std::min<int64_t>(total, WALKERS));
         });
     } else if (bcn) {
-        if (gx) hipLaunchKernelGGL(norm_many_cols_bwd_kernel<T>, dim3((unsigned)(B * cdiv64(N, 64))), dim3(1024), 0, s, x, w, g, mean, rstd, gx, N, C);
+        if (gx)
+            hipLaunchKernelGGL(norm_many_cols_bwd_kernel<T>, dim3((unsigned)(B * cdiv64(N, 64))), dim3(1024), 0, s, x, w, g, mean, rstd, gx,
+                               N, C);
         if (gw)
             hipLaunchKernelGGL(norm_many_cols_params_kernel<T>, dim3((unsigned)C, (unsigned)slices), dim3(256), 0, s, x, g, mean, rstd,
                                partials, rows, cdiv64(rows, slices), N, C);
     } else if (wide_rows(C, LANE_ELEMENTS<T>)) {
         const int W = wide_waves(C, LANE_ELEMENTS<T>), groups = 16 / W;
-        const int64_t walkers = std::min(cdiv64(rows, groups), std::max<int64_t>(2 * device_cu_count(), cdiv64(rows, 16 * groups)));
-        const dim3 wg(64 * W * groups), grid((unsigned)(gw ? slices : std::min(walkers, WALKERS)));
-        if (!gw) hipLaunchKernelGGL((norm_wide_rows_bwd_kernel<T, false, true, 2>), grid, wg, 0, s, x, w, g, mean, rstd, gx, partials, rows, C, W);
-        else if (gx) hipLaunchKernelGGL((norm_wide_rows_bwd_kernel<T, true, true, 3>), grid, wg, 0, s, x, w, g, mean, rstd, gx, partials, rows, C, W);
-        else hipLaunchKernelGGL((norm_wide_rows_bwd_kernel<T, true, false, 3>), grid, wg, 0, s, x, w, g, mean, rstd, gx, partials, rows, C, W);
+        auto launch = [&](auto params, auto grad_x, auto deep, int64_t workgroups) {
+            hipLaunchKernelGGL((norm_wide_rows_bwd_kernel<T, decltype(params)::value, decltype(grad_x)::value, decltype(deep)::value>),
+                               dim3((unsigned)workgroups), dim3(64 * W * groups), 0, s, x, w, g, mean, rstd, gx, partials, rows, C, W);
+        };
+        const std::integral_constant<int, 2> two;
+        const std::integral_constant<int, 3> three;
+        if (gw && gx) launch(std::true_type{}, std::true_type{}, three, slices);
+        else if (gw) launch(std::true_type{}, std::false_type{}, three, slices);
+        else
+            launch(std::false_type{}, std::true_type{}, two,
+                   std::min({cdiv64(rows, groups), std::max<int64_t>(2 * device_cu_count(), cdiv64(rows, 16 * groups)), WALKERS}));
     } else if (!with_row_threads<T>(C, [&](auto l, auto u) {
                    constexpr int L = decltype(l)::value, U = decltype(u)::value;
-                   if constexpr (U == 1 || L == 1024) {
-                   constexpr int WG = rows_bwd_threads(L);
-                   const dim3 wg(WG), grid((unsigned)(gw ? slices : std::min(cdiv64(rows, WG / L), WALKERS)));
-                   auto launch = [&](auto params, auto narrow) {
-                       hipLaunchKernelGGL((norm_rows_bwd_kernel<T, L, U, decltype(params)::value, decltype(narrow)::value>), grid, wg, 0, s, x,
-                                          w, g, mean, rstd, gx, partials, rows, C);
-                   };
-                   if constexpr (L == 4)
-                       if (C < LANE_ELEMENTS<T>) {
-                           if (gw) launch(std::true_type{}, std::true_type{});
-                           else launch(std::false_type{}, std::true_type{});
-                           return;
-                       }
-                   if (gw) launch(std::true_type{}, std::false_type{});
-                   else launch(std::false_type{}, std::false_type{});
+                   if constexpr ((L <= 32 && U == 1) || L == 1024) {       // (the others are wide rows)
+                       constexpr int WG = rows_bwd_threads(L);
+                       const dim3 wg(WG), grid((unsigned)(gw ? slices : std::min(cdiv64(rows, WG / L), WALKERS)));
+                       auto launch = [&](auto params, auto narrow) {
+                           hipLaunchKernelGGL((norm_rows_bwd_kernel<T, L, U, decltype(params)::value, decltype(narrow)::value>), grid, wg, 0,
+                                              s, x, w, g, mean, rstd, gx, partials, rows, C);
+                       };
+                       if constexpr (L == 4)
+                           if (C < LANE_ELEMENTS<T>) {
+                               if (gw) launch(std::true_type{}, std::true_type{});
+                               else launch(std::false_type{}, std::true_type{});
+                               return;
+                           }
+                       if (gw) launch(std::true_type{}, std::false_type{});
+                       else launch(std::false_type{}, std::false_type{});
                    }
                })) {
         if (gx) hipLaunchKernelGGL(norm_long_rows_bwd_kernel<T>, dim3((unsigned)rows), dim3(1024), 0, s, x, w, g, mean, rstd, gx, C);
@@ -970,8 +983,13 @@ static hipError_t launch_norm_bwd(const T *x, const void *weight, const T *g, co
                                mean, rstd, partials, rows, cdiv64(rows, slices), C);
     }
     if (gw) {
-        if (2 * C >= 64 * 64) hipLaunchKernelGGL(norm_params_sum_kernel<64>, dim3((unsigned)(2 * C + 63) / 64), dim3(1024), 0, s, partials, slices, gw, gb, C, pdtype);
-        else hipLaunchKernelGGL(norm_params_sum_kernel<16>, dim3((unsigned)(2 * C + 15) / 16), dim3(1024), 0, s, partials, slices, gw, gb, C, pdtype);
+        auto launch = [&](auto columns) {
+            constexpr int COLUMNS = decltype(columns)::value;
+            hipLaunchKernelGGL(norm_params_sum_kernel<COLUMNS>, dim3((unsigned)(2 * C + COLUMNS - 1) / COLUMNS), dim3(1024), 0, s, partials,
+                               slices, gw, gb, C, pdtype);
+        };
+        if (2 * C >= 64 * 64) launch(std::integral_constant<int, 64>{});
+        else launch(std::integral_constant<int, 16>{});
     }
     return hipGetLastError();
 }
