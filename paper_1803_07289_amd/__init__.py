@@ -668,6 +668,8 @@ def _here(t, name):
 
 def _any(t, name, dtypes=_DTYPES):
     """_dev for a tensor of one of the types `dtypes`, on the current device."""
+    if isinstance(t, torch.Tensor) and t.is_cuda and t.get_device() == _current() and t.dtype in dtypes and t.is_contiguous():
+        return t                # (one line: a small call's checks take as long as its kernel)
     _here(t, name)
     if t.dtype not in dtypes:
         raise TypeError(f"{name} must be one of {', '.join(str(d) for d in dtypes)}, got {t.dtype}")
@@ -702,8 +704,7 @@ def flexnorm_fwd(x, weight=None, bias=None, eps=1e-5, layout=BCN, out=None):
         out = torch.empty_like(x)
     elif _any(out, "out", (x.dtype,)).shape != x.shape:
         raise ValueError("out has the wrong shape")
-    stats = torch.empty((2, B, N), dtype=torch.float32, device=x.device)
-    mean, rstd = stats.unbind(0)
+    mean, rstd = x.new_empty((2, B, N), dtype=torch.float32).unbind(0)
     _check(lib().flexnorm_fwd(_ptr(x), _ptr(weight), _ptr(bias), _ptr(out), _ptr(mean), _ptr(rstd), B, N, C, eps, _DTYPES[x.dtype],
                               0 if weight is None else _DTYPES[weight.dtype], layout, _stream()), "flexnorm_fwd")
     return out, mean, rstd
@@ -769,15 +770,13 @@ def flexlogp_fwd(logits, target=None, top=0, layout=BCN, workspace=None):
     need = lib().flexlogp_fwd_workspace_bytes(B, N, C, top, _DTYPES[logits.dtype], layout)
     if need == 0:
         raise ValueError(f"flexlogp_fwd does not take B={B}, N={N}, C={C}, top={top}")
-    stats = torch.empty((3, B, N), dtype=torch.float32, device=logits.device)
-    logp, entropy, lse = stats.unbind(0)
+    logp, entropy, lse = logits.new_empty((3, B, N), dtype=torch.float32).unbind(0)
     if target is None:
         logp = None
     top_logp = top_class = None
     if top:
         shape = (B, top, N) if layout == BCN else (B, N, top)
-        top_logp = torch.empty(shape, dtype=torch.float32, device=logits.device)
-        top_class = torch.empty(shape, dtype=torch.int32, device=logits.device)
+        top_logp, top_class = logits.new_empty(shape, dtype=torch.float32), logits.new_empty(shape, dtype=torch.int32)
     ws, ws_bytes = _ws_arg(workspace, logits.device, need) if need > _LOGP_NO_WORKSPACE else (None, 0)
     _check(lib().flexlogp_fwd(_ptr(logits), _ptr(target), _ptr(logp), _ptr(entropy), _ptr(lse), _ptr(top_logp), _ptr(top_class),
                               B, N, C, top, row, _DTYPES[logits.dtype], layout, _ptr(ws), ws_bytes, _stream()), "flexlogp_fwd")
@@ -800,7 +799,7 @@ def flexlogp_bwd(logits, target, lse, entropy, grad_logp, grad_entropy=None, lay
         if tuple(_any(t, name, _F32).shape) != (B, N):
             raise ValueError(f"{name} must be [B,N]")
     if out is None:
-        out = torch.empty(logits.shape, dtype=logits.dtype, device=logits.device)
+        out = torch.empty_like(logits, memory_format=torch.contiguous_format)
         grad_row = logits.shape[2]
     else:
         grad_row = _score_dims(out, layout, "out")[3]
