@@ -5,8 +5,8 @@
 // A score of -inf has p = 0 and no share of anything; positions whose target is no class are ignored (outputs zero, no
 // alternatives, gradient zero, scores not looked at); one without any score above -inf has logp = lse = -inf, H = 0.
 //
-// Every kernel reads a score once and keeps it in a register, fp32 or packed as it was, until its position is done: the maximum, the
-// two sums and the alternatives all come from there.
+// A score is read once and kept in a register until its position is done: the maximum, the two sums and the alternatives all come from
+// there.  Of positions too long for that, a part's running sums are kept, and what may be among the best is read again.
 #include "flex_elem.hpp"
 #include <algorithm>
 
