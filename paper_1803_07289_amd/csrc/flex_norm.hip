@@ -581,97 +581,115 @@ __global__ __launch_bounds__(256) void norm_long_rows_params_kernel(const T *__r
 }
 
 // ---- channel-major ----------------------------------------------------------------------------------------------------------
-// A lane to a position, W waves of a workgroup share the channels: R of them a wave in registers, or (R = 0) any number, read again.
-// Bound by memory; 16-bit types, of which a wave loads half a line at a time, by the number of loads.  us, x of 168 MB, forward and backward: fp32,
-// 16 channels 82 and 134, 64 82 and 142, 200 80 and 119, 400 130 and 243; bf16, 16 channels 105 and 159, 64 114 and 176, 200 116 and 149.
+// A lane to P positions, W waves of a workgroup share the channels: R of them a wave in registers, or (R = 0) any number, read again.
+// P = 2 of 16 bits, so that a wave's loads are whole lines.
+// Bound by memory.  us, x of 168 MB, forward and backward: fp32, 16 channels 81 and 133, 64 83 and 140, 200 81 and 116, 400 130 and 243; bf16,
+// 16 channels 88 and 137 (a position to a lane 105 and 158), 64 87 and 143 (113 and 171), 200 91 and 149 (115 and 149), 400 158 and 320.
 constexpr int COL_CHANNELS = 16;
 
 // sums over the waves of a workgroup, by position
-template <int W>
-__device__ __forceinline__ float waves_sum(float v, float (*place)[64])
+template <int W, int P>
+__device__ __forceinline__ void waves_sum(float (&v)[P], float (*place)[P][64])
 {
-    if (W == 1) return v;
+    if (W == 1) return;
     const int lane = threadIdx.x & 63;
-    place[threadIdx.x >> 6][lane] = v;
-    __syncthreads();
-    v = place[0][lane];
 #pragma unroll
-    for (int i = 1; i < W; ++i) v += place[i][lane];
-    return v;
+    for (int q = 0; q < P; ++q) place[threadIdx.x >> 6][q][lane] = v[q];
+    __syncthreads();
+#pragma unroll
+    for (int q = 0; q < P; ++q) {
+        v[q] = place[0][q][lane];
+#pragma unroll
+        for (int i = 1; i < W; ++i) v[q] += place[i][q][lane];
+    }
 }
 
-template <class T, int W, int R>
+template <class T, int W, int R, int P>
 __global__ __launch_bounds__(64 * W) void norm_cols_kernel(const T *__restrict__ x, Param<T> w, Param<T> b, T *__restrict__ y,
                                                            float *mean_out, float *rstd_out, int N, int C, float eps)
 {
-    __shared__ float s_place[2][W][64];
+    typedef typename Chunk<T, P>::V V;
+    __shared__ float s_place[2][W][P][64];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const unsigned tiles = (unsigned)(N + 63) / 64;
+    const unsigned tiles = (unsigned)(N + 64 * P - 1) / (64 * P);
     const int64_t cloud = blockIdx.x / tiles;
-    const int n = (int)(blockIdx.x % tiles) * 64 + lane;
-    const bool mine = n < N;
+    const int n = (int)(blockIdx.x % tiles) * 64 * P + lane * P, n0 = min(n, N - P);
+    const bool mine = n < N;        // (the last of an odd number of positions: with the one before it, which another lane writes too, the same)
     const int per = R ? R : (C + W - 1) / W, first = wave * per, last = min(first + per, C);
-    const int64_t base = cloud * C * (int64_t)N + min(n, N - 1);
+    const int64_t base = cloud * C * (int64_t)N + n0;
     const float count = (float)C;
-    float v[R ? R : 1], sum = 0.f, sq = 0.f;
-    T raw[R ? R : 1];        // (all loads before the first is converted, in no branch)
+    float v[R ? R : 1][P], mean[P], rstd[P];
+    V raw[R ? R : 1];        // (all loads before the first is converted, in no branch)
+#pragma unroll
+    for (int q = 0; q < P; ++q) mean[q] = rstd[q] = 0.f;
     if (R) {
 #pragma unroll
-        for (int i = 0; i < R; ++i) raw[i] = x[base + (int64_t)min(first + i, C - 1) * N];
+        for (int i = 0; i < R; ++i) raw[i] = *(const V *)(x + base + (int64_t)min(first + i, C - 1) * N);
 #pragma unroll
-        for (int i = 0; i < R; ++i) {
-            v[i] = first + i < last ? to_f32(raw[i]) : 0.f;
-            sum += v[i];
-        }
+        for (int i = 0; i < R; ++i)
+#pragma unroll
+            for (int q = 0; q < P; ++q) {
+                v[i][q] = first + i < last ? to_f32(raw[i][q]) : 0.f;
+                mean[q] += v[i][q];
+            }
     } else
 #pragma unroll 8
-        for (int c = first; c < last; ++c) sum += to_f32(x[base + (int64_t)c * N]);
+        for (int c = first; c < last; ++c) mean[0] += to_f32(x[base + (int64_t)c * N]);
     const float ww = R && w.p && lane < last - first ? w[first + lane] : 1.f, bb = R && w.p && lane < last - first ? b[first + lane] : 0.f;
-    const float mean = waves_sum<W>(sum, s_place[0]) / count;
+    waves_sum<W, P>(mean, s_place[0]);
+#pragma unroll
+    for (int q = 0; q < P; ++q) mean[q] /= count;
     if (R) {
 #pragma unroll
-        for (int i = 0; i < R; ++i) {
-            const float d = v[i] - mean;
-            if (first + i < last) sq += d * d;
-        }
+        for (int i = 0; i < R; ++i)
+#pragma unroll
+            for (int q = 0; q < P; ++q) {
+                const float d = v[i][q] - mean[q];
+                if (first + i < last) rstd[q] += d * d;
+            }
     } else
 #pragma unroll 8
         for (int c = first; c < last; ++c) {
-            const float d = to_f32(x[base + (int64_t)c * N]) - mean;
-            sq += d * d;
+            const float d = to_f32(x[base + (int64_t)c * N]) - mean[0];
+            rstd[0] += d * d;
         }
-    const float rstd = 1.f / sqrtf(waves_sum<W>(sq, s_place[1]) / count + eps);
+    waves_sum<W, P>(rstd, s_place[1]);
+#pragma unroll
+    for (int q = 0; q < P; ++q) rstd[q] = 1.f / sqrtf(rstd[q] / count + eps);
     if (R) {
 #pragma unroll
-        for (int i = 0; i < R; ++i) v[i] = (v[i] - mean) * rstd * lane_value(ww, i) + lane_value(bb, i);
+        for (int i = 0; i < R; ++i)
+#pragma unroll
+            for (int q = 0; q < P; ++q) v[i][q] = (v[i][q] - mean[q]) * rstd[q] * lane_value(ww, i) + lane_value(bb, i);
         if (!mine) return;
 #pragma unroll
         for (int i = 0; i < R; ++i)
-            if (first + i < last) y[base + (int64_t)(first + i) * N] = (T)v[i];
+            if (first + i < last) Chunk<T, P>::store(y + base + (int64_t)(first + i) * N, v[i]);
     } else {
         if (!mine) return;
 #pragma unroll 8
         for (int c = first; c < last; ++c) {
-            const float d = (to_f32(x[base + (int64_t)c * N]) - mean) * rstd;
+            const float d = (to_f32(x[base + (int64_t)c * N]) - mean[0]) * rstd[0];
             y[base + (int64_t)c * N] = (T)(w.p ? d * w[c] + b[c] : d);
         }
     }
     if (wave == 0) {
-        if (mean_out) mean_out[cloud * N + n] = mean;
-        if (rstd_out) rstd_out[cloud * N + n] = rstd;
+        if (mean_out) Chunk<float, P>::store(mean_out + cloud * N + n0, mean);
+        if (rstd_out) Chunk<float, P>::store(rstd_out + cloud * N + n0, rstd);
     }
 }
 
-// Backward: a workgroup walks over tiles of 64 positions; a lane adds its positions' shares of grad_w and grad_b up for each of its
+// Backward: a workgroup walks over tiles of 64 P positions; a lane adds its positions' shares of grad_w and grad_b up for each of its
 // channels, the lanes of a wave meet at the end.
-template <class T, int W, bool PARAMS>
+template <class T, int W, bool PARAMS, int P>
 __global__ __launch_bounds__(64 * W) void norm_cols_bwd_kernel(const T *__restrict__ x, Param<T> w, const T *__restrict__ g,
                                                                const float *__restrict__ mean, const float *__restrict__ rstd,
                                                                T *__restrict__ gx, float *__restrict__ partials, int N, int C,
                                                                unsigned tiles, unsigned total)
 {
     constexpr int R = COL_CHANNELS;
-    __shared__ float s_place[2][2][W][64];
+    typedef typename Chunk<T, P>::V V;
+    __shared__ float s_place[2][W][2 * P][64];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int first = wave * R, many = min(R, C - first);
     const float count = (float)C;
@@ -682,36 +700,46 @@ __global__ __launch_bounds__(64 * W) void norm_cols_bwd_kernel(const T *__restri
     int turn = 0;
     for (unsigned tile = blockIdx.x; tile < total; tile += gridDim.x, turn ^= 1) {
         const int64_t cloud = tile / tiles;
-        const int n = (int)(tile % tiles) * 64 + lane;
-        const bool mine = n < N;
-        const int64_t base = (cloud * C + first) * (int64_t)N + min(n, N - 1), at = cloud * N + min(n, N - 1);
-        float xh[R], gg[R], s1 = 0.f, s2 = 0.f;
-        T xr[R], gr[R];
+        const int n = (int)(tile % tiles) * 64 * P + lane * P, n0 = min(n, N - P);
+        const int64_t base = (cloud * C + first) * (int64_t)N + n0, at = cloud * N + n0;
+        V xr[R], gr[R];
 #pragma unroll
         for (int i = 0; i < R; ++i) {
-            xr[i] = x[base + (int64_t)min(i, many - 1) * N];
-            gr[i] = g[base + (int64_t)min(i, many - 1) * N];
+            xr[i] = *(const V *)(x + base + (int64_t)min(i, many - 1) * N);
+            gr[i] = *(const V *)(g + base + (int64_t)min(i, many - 1) * N);
         }
-        const float m = mean[at], r = rstd[at];
+        float m[P], r[P], s[2 * P];
+        Chunk<float, P>::load(mean + at, m);
+        Chunk<float, P>::load(rstd + at, r);
 #pragma unroll
-        for (int i = 0; i < R; ++i) {
-            xh[i] = (to_f32(xr[i]) - m) * r;
-            gg[i] = i < many && mine ? to_f32(gr[i]) : 0.f;
-            const float h = gg[i] * lane_value(ww, i);
-            s1 += h;
-            s2 += h * xh[i];
-            if (PARAMS) {
-                gw[i] += gg[i] * xh[i];
-                gb[i] += gg[i];
+        for (int q = 0; q < 2 * P; ++q) s[q] = 0.f;
+#pragma unroll
+        for (int i = 0; i < R; ++i)
+#pragma unroll
+            for (int q = 0; q < P; ++q) {
+                const float xh = (to_f32(xr[i][q]) - m[q]) * r[q], gg = i < many ? to_f32(gr[i][q]) : 0.f, h = gg * lane_value(ww, i);
+                s[q] += h;
+                s[P + q] += h * xh;
+                if (PARAMS) {
+                    const float own = n0 + q >= n ? gg : 0.f;        // (another lane counts a position before n; behind the last there is none)
+                    gw[i] += own * xh;
+                    gb[i] += own;
+                }
             }
-        }
         if (PARAMS && !gx) continue;
-        s1 = waves_sum<W>(s1, s_place[turn][0]) / count;
-        s2 = waves_sum<W>(s2, s_place[turn][1]) / count;
+        waves_sum<W, 2 * P>(s, s_place[turn]);
+#pragma unroll
+        for (int q = 0; q < 2 * P; ++q) s[q] /= count;
 #pragma unroll
         for (int i = 0; i < R; ++i) {
-            const float out = (gg[i] * lane_value(ww, i) - s1 - xh[i] * s2) * r;
-            if (i < many && mine) gx[base + (int64_t)i * N] = (T)out;
+            if (P > 1) asm("" : "+v"(xr[i]), "+v"(gr[i]));       // converted again here, and not kept from above
+            float out[P];
+#pragma unroll
+            for (int q = 0; q < P; ++q) {
+                const float xh = (to_f32(xr[i][q]) - m[q]) * r[q];
+                out[q] = (to_f32(gr[i][q]) * lane_value(ww, i) - s[q] - xh * s[P + q]) * r[q];
+            }
+            if (i < many && n < N) Chunk<T, P>::store(gx + base + (int64_t)i * N, out);
         }
     }
     if (!PARAMS) return;
@@ -732,7 +760,7 @@ __global__ __launch_bounds__(1024) void norm_many_cols_bwd_kernel(const T *__res
                                                                   T *__restrict__ gx, int N, int C)
 {
     constexpr int W = 16;
-    __shared__ float s_place[2][W][64];
+    __shared__ float s_place[W][2][64];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const unsigned tiles = (unsigned)(N + 63) / 64;
     const int64_t cloud = blockIdx.x / tiles;
@@ -747,8 +775,10 @@ __global__ __launch_bounds__(1024) void norm_many_cols_bwd_kernel(const T *__res
         s1 += h;
         s2 += h * ((to_f32(x[base + (int64_t)c * N]) - m) * r);
     }
-    s1 = waves_sum<W>(s1, s_place[0]) / count;
-    s2 = waves_sum<W>(s2, s_place[1]) / count;
+    float s[2] = {s1, s2};
+    waves_sum<W, 2>(s, s_place);
+    s1 = s[0] / count;
+    s2 = s[1] / count;
     if (n >= N) return;
 #pragma unroll 8
     for (int c = first; c < last; ++c) {
@@ -848,6 +878,15 @@ static void with_col_waves(int C, F f)
     else f(std::integral_constant<int, 16>{});
 }
 
+// f(P): positions to a lane, channel-major: two of 16 bits, so that a wave's loads are whole lines
+template <class T, class F>
+static void with_positions(int N, F f)
+{
+    if constexpr (sizeof(T) == 2)
+        if (N >= 2) return f(std::integral_constant<int, 2>{});
+    f(std::integral_constant<int, 1>{});
+}
+
 // Rows of more than 32 lanes of 16 bytes, up to 16 waves: the backward pass has a kernel for them.
 static bool wide_rows(int C, int lane) { return C > 32 * lane && C <= 1024 * lane; }
 static int wide_waves(int C, int lane) { return (C + 64 * lane - 1) / (64 * lane); }
@@ -879,7 +918,7 @@ static int norm_slices(int B, int N, int C, int dtype, bool bcn)
     if (bcn) {
         if (C > COL_CHANNELS_MAX) return (int)std::min<int64_t>(64, cdiv64(rows, 4096));
         const int64_t waves = cdiv64(C, COL_CHANNELS);
-        return (int)std::min<int64_t>(B * cdiv64(N, 64), std::max<int64_t>(cus, 8 * cus / waves));
+        return (int)std::min<int64_t>(B * cdiv64(N, dtype == FLEX_F32 || C > 8 * COL_CHANNELS ? 64 : 128), std::max<int64_t>(cus, 8 * cus / waves));
     }
     if (C > ROW_CHANNELS_MAX) return (int)std::min<int64_t>(64, cdiv64(rows, 16));
     const int lane = 16 / (int)dtype_bytes(dtype);
@@ -896,14 +935,19 @@ static hipError_t launch_norm_fwd(const T *x, const void *weight, const void *bi
     const int64_t rows = (int64_t)B * N;
     const Param<T> w{weight, pdtype == FLEX_F32}, b{bias, pdtype == FLEX_F32};
     if (bcn) {
-        const dim3 grid((unsigned)(B * cdiv64(N, 64)));
-        if (C > COL_CHANNELS_MAX)
-            hipLaunchKernelGGL((norm_cols_kernel<T, 16, 0>), grid, dim3(1024), 0, s, x, w, b, y, mean, rstd, N, C, eps);
-        else
-            with_col_waves(C, [&](auto waves) {
-                constexpr int W = decltype(waves)::value;
-                hipLaunchKernelGGL((norm_cols_kernel<T, W, COL_CHANNELS>), grid, dim3(64 * W), 0, s, x, w, b, y, mean, rstd, N, C, eps);
+        if (C > COL_CHANNELS_MAX) {
+            hipLaunchKernelGGL((norm_cols_kernel<T, 16, 0, 1>), dim3((unsigned)(B * cdiv64(N, 64))), dim3(1024), 0, s, x, w, b, y, mean, rstd, N, C,
+                               eps);
+            return hipGetLastError();
+        }
+        with_col_waves(C, [&](auto waves) {
+            constexpr int W = decltype(waves)::value;
+            with_positions<T>(N, [&](auto positions) {
+                constexpr int P = decltype(positions)::value;
+                hipLaunchKernelGGL((norm_cols_kernel<T, W, COL_CHANNELS, P>), dim3((unsigned)(B * cdiv64(N, 64 * P))), dim3(64 * W), 0, s, x, w, b,
+                                   y, mean, rstd, N, C, eps);
             });
+        });
         return hipGetLastError();
     }
     if (!with_row_threads<T>(C, [&](auto l, auto u) {
@@ -928,15 +972,18 @@ static hipError_t launch_norm_bwd(const T *x, const void *weight, const T *g, co
     const Param<T> w{weight, pdtype == FLEX_F32};
     const int slices = norm_slices(B, N, C, dtype, bcn);
     if (bcn && C <= COL_CHANNELS_MAX) {
-        const unsigned tiles = (unsigned)(N + 63) / 64, total = (unsigned)B * tiles;
         with_col_waves(C, [&](auto waves) {
             constexpr int W = decltype(waves)::value;
-            auto launch = [&](auto params, int64_t workgroups) {
-                hipLaunchKernelGGL((norm_cols_bwd_kernel<T, W, decltype(params)::value>), dim3((unsigned)workgroups), dim3(64 * W), 0, s, x, w, g,
-                                   mean, rstd, gx, partials, N, C, tiles, total);
+            auto launch = [&](auto params, auto positions) {
+                constexpr int P = decltype(positions)::value;
+                const unsigned tiles = (unsigned)(N + 64 * P - 1) / (64 * P), total = (unsigned)B * tiles;
+                const int64_t workgroups = gw ? slices : std::min<int64_t>(total, WALKERS);
+                hipLaunchKernelGGL((norm_cols_bwd_kernel<T, W, decltype(params)::value, P>), dim3((unsigned)workgroups), dim3(64 * W), 0, s, x, w,
+                                   g, mean, rstd, gx, partials, N, C, tiles, total);
             };
-            if (gw) launch(std::true_type{}, slices);
-            else launch(std::false_type{}, std::min<int64_t>(total, WALKERS));
+            if (!gw) with_positions<T>(N, [&](auto positions) { launch(std::false_type{}, positions); });
+            else if constexpr (W == 16) launch(std::true_type{}, std::integral_constant<int, 1>{});       // (two, and the sums do not fit the registers)
+            else with_positions<T>(N, [&](auto positions) { launch(std::true_type{}, positions); });
         });
     } else if (bcn) {
         if (gx)
