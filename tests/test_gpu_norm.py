@@ -137,6 +137,33 @@ def test_large_sums_over_positions():
             assert bool((off <= kr * terms.abs().sum(rows)).all())
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("layout, C, N", [(fx.BCN, 100, 90_001), (fx.BCN, 20, 300_002), (fx.BCN, 250, 30_003), (fx.BNC, 600, 20_005),
+                                          (fx.BNC, 40, 150_001)])
+def test_workgroups_that_walk_over_many_positions(layout, C, N, dtype):
+    """Every turn of the backward kernels' loops; the reference on the GPU in float64 from the same statistics."""
+    g = torch.Generator(device="cuda").manual_seed(C)
+    shape = (1, C, N) if layout == fx.BCN else (1, N, C)
+    d = 1 if layout == fx.BCN else 2
+    x, go = (torch.randn(shape, device="cuda", generator=g).to(TYPES[dtype]) for _ in range(2))
+    w = torch.rand(C, device="cuda", generator=g) + 0.5
+    _, mean, rstd = fx.flexnorm_fwd(x, w, w, layout=layout)
+    gx, gw, gb = fx.flexnorm_bwd(x, w, go, mean, rstd, layout=layout)
+    r = rstd.double().unsqueeze(d)
+    xh = (x.double() - mean.double().unsqueeze(d)) * r
+    rows = (0, 3 - d)
+    for got, terms in ((gw, go.double() * xh), (gb, go.double())):
+        assert bool(((got.double() - terms.sum(rows)).abs() <= chain(N, 256) * terms.abs().sum(rows)).all())
+    h = go.double() * (w.double()[:, None] if layout == fx.BCN else w.double())
+    m1, m2 = h.mean(d, keepdim=True), (h * xh).mean(d, keepdim=True)
+    want = r * (h - m1 - xh * m2)
+    part = h.abs() + h.abs().mean(d, keepdim=True) + 2 * xh.abs() * (h * xh).abs().mean(d, keepdim=True)
+    bound = chain(C) * r * part + half_step(TYPES[dtype]) * want.abs() + smallest_half(TYPES[dtype])
+    assert bool(((gx.double() - want).abs() <= bound).all())
+    only = fx.flexnorm_bwd(x, w, go, mean, rstd, layout=layout, need_params=False)[0]
+    assert bool(((only.double() - want).abs() <= bound).all())
+
+
 def test_refusals_of_the_binding():
     x, w = torch.zeros(2, 5, 8, device="cuda"), torch.zeros(5, device="cuda")
     y, mean, rstd = fx.flexnorm_fwd(x, w, w)
