@@ -24,6 +24,9 @@ struct LogpArgs {
     int N, C, top;
 };
 
+// A maximum of a number and a NaN is the number, also if the NaN signals: the mode register's bit 9 off, for the wave.
+__device__ __forceinline__ void maxima_of_numbers() { __builtin_amdgcn_s_setreg(1 | 9 << 6, 0); }
+
 struct Sums {
     float m, s, u;
 };
@@ -190,6 +193,7 @@ __global__ __launch_bounds__(256) void logp_rows_kernel(const T *__restrict__ x,
 {
     constexpr int N = LANE_ELEMENTS<T>;
     __shared__ Candidate s_list[L == 64 ? 4 : 1][ROW_LIST];
+    maxima_of_numbers();
     const int sub = threadIdx.x % L;
     const int64_t row = (int64_t)blockIdx.x * (256 / L) + threadIdx.x / L;
     const bool mine = row < a.rows;
@@ -361,6 +365,7 @@ __global__ __launch_bounds__(256) void logp_part_kernel(const T *__restrict__ x,
 {
     constexpr int N = LANE_ELEMENTS<T>, U = SPAN_LOADS, GROUPS = U * N / 4;
     typedef typename Chunk<T>::V V;
+    maxima_of_numbers();
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const unsigned part = blockIdx.x % p.parts;
     const int64_t row = blockIdx.x / p.parts;
@@ -604,6 +609,7 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void logp_lanes_kernel(const
     __shared__ Sums s_sums[W][64];
     __shared__ float s_best[W][64];
     __shared__ int s_class[W][64];
+    maxima_of_numbers();
     const int lane = threadIdx.x & 63, wave = W == 1 ? 0 : threadIdx.x >> 6;
     const unsigned tile = W == 1 ? blockIdx.x * 4 + (threadIdx.x >> 6) : blockIdx.x, tiles = ROWS ? 1u : (unsigned)(a.N + 63) / 64;
     const int64_t b = ROWS ? 0 : tile / tiles;

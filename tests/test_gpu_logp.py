@@ -180,6 +180,23 @@ def test_nan_and_infinity_among_the_scores(C, layout):
         torch.from_numpy(to_positions(v, layout)[[0, 3]])[None] for v in got[3:]), 4, fx.BNC)
 
 
+@pytest.mark.parametrize("layout", [fx.BNC, fx.BCN], ids=["bnc", "bcn"])
+@pytest.mark.parametrize("dtype, bits", [("f32", 0x7F800001), ("bf16", 0x7F81), ("f16", 0x7C01)])
+@pytest.mark.parametrize("C", [9, 30, 200, 3000, 70000])
+def test_signalling_nan_among_the_scores(C, dtype, bits, layout):
+    """No alternative, and no cover for its neighbours: the best score lies beside one, the next further on."""
+    _, x = scores(5, 6, C, TYPES[dtype])
+    x[:, C // 2] = 40.0
+    x[:, C // 4] = 30.0
+    dx = laid_out(x, 1, layout, TYPES[dtype])
+    raw = dx.view(torch.int32 if dtype == "f32" else torch.int16)
+    for c in (C // 2 - 1, C // 2 + 1):
+        (raw[:, :, c] if layout == fx.BNC else raw[:, c, :]).fill_(bits)
+    got = fx.flexlogp_fwd(dx, top=2, layout=layout)
+    assert torch.isnan(got[1]).all() and torch.isnan(got[2]).all()
+    assert (to_positions(got[4], layout) == [C // 2, C // 4]).all()
+
+
 def test_scores_of_the_types_extremes():
     big = float(torch.finfo(torch.float32).max)
     x = np.array([[-big, 0.0, 1.0, -big], [-big] * 4, [big, big, 0.0, -big], [88.0, -88.0, 700.0, 699.0]])
