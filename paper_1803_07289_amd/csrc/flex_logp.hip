@@ -15,6 +15,9 @@ namespace flex {
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 constexpr float MASKED = -1e5f;       // stands for x - m = -inf where it is multiplied by exp(x - m) = 0
 constexpr int NO_CLASS = 0x7FFFFFFF;
+// Up to this maximum exp(x - m) is 2^(x log2(e) - shift), one fused operation, with shift = m log2(e) rounded: the sums are then about the
+// shift, and delta = m log2(e) - shift, up to 2^-8 here, is taken out of them once they are finished.  Above it, the difference first.
+constexpr float SHIFT_MAX = 65536.f;
 
 struct LogpArgs {
     const int32_t *target;
@@ -55,10 +58,19 @@ __device__ __forceinline__ void add_score(Sums &a, float x, float m)
     a.s += e;
     a.u += e * fmaxf(z, MASKED);
 }
+// what m log2(e) is more than its rounded value
+__device__ __forceinline__ float shift_error(float m, float shift) { return __builtin_fmaf(m, LOG2E, -shift); }
+// ln of the sum about its largest score, whose own term is 1: never below 0, where rounding alone would take it (no score: -inf)
+__device__ __forceinline__ float log_sum(float s, float away = 0.f)
+{
+    const float l = logf(s) - away;
+    return l < 0.f && s > 0.f ? 0.f : l;
+}
 __device__ __forceinline__ void store_sums(const LogpArgs &a, int64_t row, float target_score, const Sums &k, float log_s)
 {
     if (a.target) a.logp[row] = k.s == 0.f ? -INFINITY : target_score - k.m - log_s;
-    a.entropy[row] = k.s == 0.f ? 0.f : log_s - k.u / k.s;
+    const float h = log_s - k.u / k.s;
+    a.entropy[row] = k.s == 0.f || h < 0.f ? 0.f : h;
     a.lse[row] = k.m + log_s;
 }
 struct Alternative {
@@ -222,8 +234,10 @@ __global__ __launch_bounds__(256) void logp_rows_kernel(const T *__restrict__ x,
     const float own_best = best;
     best = lanes_max<L>(best);
     Sums k{centre(best), 0.f, 0.f};
-    if (!__any(fabsf(k.m) > HUGE_SCORE)) {
+    float away = 0.f;       // what the sums are about is so far below m
+    if (!__any(fabsf(k.m) > SHIFT_MAX)) {
         const float shift = k.m * LOG2E;
+        away = shift_error(k.m, shift) * LN2;
 #pragma unroll
         for (int u = 0; u < U; ++u)
 #pragma unroll
@@ -241,7 +255,8 @@ __global__ __launch_bounds__(256) void logp_rows_kernel(const T *__restrict__ x,
     }
     k.s = lanes_sum<L>(k.s);
     k.u = lanes_sum<L>(k.u);
-    const float log_s = logf(k.s);
+    k.u = __builtin_fmaf(-away, k.s, k.u);      // (of both only the quotient is used, and ln s)
+    const float log_s = log_sum(k.s, away);
     if (mine && sub == 0) {
         if (skip) {
             a.logp[row] = a.entropy[row] = a.lse[row] = 0.f;
