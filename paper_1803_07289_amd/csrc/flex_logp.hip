@@ -58,6 +58,12 @@ __device__ __forceinline__ void add_score(Sums &a, float x, float m)
     a.s += e;
     a.u += e * fmaxf(z, MASKED);
 }
+// m log2(e), rounded: nothing that is subtracted from it is fused with the product
+__device__ __forceinline__ float rounded_shift(float m)
+{
+#pragma clang fp contract(off)
+    return m * LOG2E;
+}
 // what m log2(e) is more than its rounded value
 __device__ __forceinline__ float shift_error(float m, float shift) { return __builtin_fmaf(m, LOG2E, -shift); }
 // ln of the sum about its largest score, whose own term is 1: never below 0, where rounding alone would take it (no score: -inf)
@@ -174,7 +180,7 @@ constexpr int SUMS_BYTES = 16, SPAN_LOADS = 4;
 template <class T>
 constexpr int SPAN = 256 * LANE_ELEMENTS<T> * SPAN_LOADS;     // elements that a workgroup takes at a time: 16 KB
 
-constexpr float LOWEST = -3.4028234663852886e38f, HUGE_SCORE = 1e37f;
+constexpr float LOWEST = -3.4028234663852886e38f;
 constexpr int WAVE_LIST = 64 * 4 + FLEX_LOGP_MAX_TOP, LISTS_JOINED = 512;
 
 __device__ __forceinline__ float max3(float a, float b, float c)
@@ -236,7 +242,7 @@ __global__ __launch_bounds__(256) void logp_rows_kernel(const T *__restrict__ x,
     Sums k{centre(best), 0.f, 0.f};
     float away = 0.f;       // what the sums are about is so far below m
     if (!__any(fabsf(k.m) > SHIFT_MAX)) {
-        const float shift = k.m * LOG2E;
+        const float shift = rounded_shift(k.m);
         away = shift_error(k.m, shift) * LN2;
 #pragma unroll
         for (int u = 0; u < U; ++u)
@@ -365,7 +371,8 @@ __global__ __launch_bounds__(256) void logp_rows_kernel(const T *__restrict__ x,
 // A workgroup runs along a part of a row, 16 KB at a time, the next 16 KB on their way meanwhile.  A lane's sums are about its own
 // maximum so far and meet at the end.  What an element costs decides beside the memory (bf16: 2 bytes in the time of some 11 vector
 // operations): exp counts four, the product and difference in front of it are one fused operation, the maximum takes two elements a
-// step.
+// step.  A lane's sums are about its maximum's rounded shift while the wave has met none above SHIFT_MAX, then about the maximum itself, as
+// all are when they meet.
 // Alternatives: the `top`-th largest of the 64 maxima that four lanes each have met so far is reached by `top` scores of the part, so
 // only what reaches it can be among the best; that goes to the wave's list in LDS.  The bound is found after the first span and
 // renewed when as many again have passed, from whatever maxima the other waves have left by then: each is a score of the part,
@@ -411,6 +418,13 @@ __global__ __launch_bounds__(256) void logp_part_kernel(const T *__restrict__ x,
     request(begin);
     const float target_score = tid == 0 && a.target && p.parts == 1 ? to_f32(at[t]) : 0.f;
     Sums k{-INFINITY, 0.f, 0.f};       // of the lane; u in units of ln 2
+    float about = -INFINITY;           // the shift that they are about, unless the wave is far
+    bool far = false;
+    const auto about_maximum = [&]() {
+        const float m = centre(k.m), d = shift_error(m, rounded_shift(m)), e = __builtin_amdgcn_exp2f(-d);
+        k.u = __builtin_fmaf(-d, k.s, k.u) * e;
+        k.s *= e;
+    };
     float least = LOWEST, bound = LOWEST;       // what a candidate reaches; what `top` scores of the part are known to reach
     float last = -INFINITY;            // the least of the list when it was last cut
     int count = 0, renew = begin;      // the wave's list; where its bound is due
@@ -448,18 +462,21 @@ __global__ __launch_bounds__(256) void logp_part_kernel(const T *__restrict__ x,
             most[g] = max3(max3(w[0], w[1], w[2]), w[3], -INFINITY);
             span_most = fmaxf(span_most, most[g]);
         }
-        const float was = k.m;
-        k.m = fmaxf(was, span_most);
-        const float m = centre(k.m);
-        const bool far = __any(fabsf(m) > HUGE_SCORE);       // m log2(e) may be no number of fp32: the difference first
+        const float was = k.m, now = fmaxf(was, span_most), m = centre(now), was_about = about;
+        if (!far && __any(fabsf(m) > SHIFT_MAX)) {
+            about_maximum();
+            far = true;
+        }
+        k.m = now;
+        about = rounded_shift(now);
+        const float shift = centre(about);
         {
-            const float d = fmaxf((was - m) * LOG2E, MASKED), e = __builtin_amdgcn_exp2f(d);
+            const float d = fmaxf(far ? (was - m) * LOG2E : was_about - shift, MASKED), e = __builtin_amdgcn_exp2f(d);
             k.u = (k.u + k.s * d) * e;
             k.s *= e;
         }
         float s[2] = {0.f, 0.f}, q[2] = {0.f, 0.f};
         if (!far) {
-            const float shift = m * LOG2E;
 #pragma unroll
             for (int u = 0; u < U; ++u)
 #pragma unroll
@@ -512,6 +529,7 @@ __global__ __launch_bounds__(256) void logp_part_kernel(const T *__restrict__ x,
         if (least == last) least = from_order_key(order_key(last) + 1);
     }
     if (count > LISTS_JOINED / 4) cut();
+    if (!far) about_maximum();
     Sums all{lanes_max<64>(k.m), 0.f, 0.f};
     {
         const float d = fmaxf((k.m - centre(all.m)) * LOG2E, MASKED), e = __builtin_amdgcn_exp2f(d);
@@ -526,7 +544,7 @@ __global__ __launch_bounds__(256) void logp_part_kernel(const T *__restrict__ x,
     __syncthreads();
     k = joined(s_sums);
     k.m = p.parts == 1 ? centre(k.m) : k.m;
-    const float log_s = logf(k.s);
+    const float log_s = log_sum(k.s);
     if (tid == 0) {
         if (p.parts == 1) store_sums(a, row, target_score, k, log_s);
         else *(Sums *)((char *)p.sums + (row * p.parts + part) * SUMS_BYTES) = k;
@@ -575,7 +593,7 @@ __global__ __launch_bounds__(64) void logp_join_kernel(const T *__restrict__ x, 
     const float m = centre(lanes_max<64>(k.m));
     const float d = fmaxf(k.m - m, MASKED), e = __builtin_amdgcn_exp2f(d * LOG2E);
     k = Sums{m, lanes_sum<64>(k.s * e), lanes_sum<64>((k.u + k.s * d) * e)};
-    const float log_s = logf(k.s);
+    const float log_s = log_sum(k.s);
     if (lane == 0) store_sums(a, row, target_score, k, log_s);
     if (a.top == 0) return;
     const float least = reached_by(looked_at ? score_of(looked_at) : -INFINITY, a.top);

@@ -92,8 +92,23 @@ def test_scores_of_any_size(C, dtype, layout):
         check(x, t, fx.flexlogp_fwd(dx, dt, top=top, layout=layout), top, layout)
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("C, times", [(5000, 1), (9000, 1), (9000, 20), (20000, 1), (70000, 1), (70000, 20), (131072, 1)])
+def test_scores_of_any_size_in_long_rows(C, times, dtype):
+    """Rows in parts; many times over, a workgroup to each."""
+    say(f"logp large scores {C} {times} {dtype}")
+    x, t = rows_of_all_sizes(C, TYPES[dtype])
+    dx, dt = laid_out(x, 1, fx.BNC, TYPES[dtype]), torch.from_numpy(t.astype(np.int32))[None].cuda()
+    if times > 1:
+        dx, dt = dx.repeat(1, times, 1), dt.repeat(1, times)
+    got = fx.flexlogp_fwd(dx, dt, top=5, layout=fx.BNC)
+    check(x, t, [v[:, :len(x)] for v in got], 5, fx.BNC)
+    for v in got:
+        assert all(torch.equal(v[:, i * len(x):(i + 1) * len(x)], v[:, :len(x)]) for i in range(times))
+
+
 @pytest.mark.parametrize("layout", [fx.BNC, fx.BCN], ids=["bnc", "bcn"])
-@pytest.mark.parametrize("C", [13, 40, 1000])
+@pytest.mark.parametrize("C", [13, 40, 1000, 3000, 70000])
 def test_a_shift_of_all_scores_changes_nothing(C, layout):
     """Scores in steps of 1/8, to which whole numbers are added without rounding: the same logp, entropy and alternatives."""
     rng = np.random.default_rng(C + 1)
