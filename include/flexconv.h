@@ -462,8 +462,9 @@ int flexlogp_fwd(const void *logits, const int32_t *target, float *logp, float *
 
 /*
  * Gradient of the scores from those of logp and of entropy (either may be NULL; grad_logp needs target, grad_entropy needs entropy),
- * lse and entropy as the forward pass left them:
+ * lse and entropy as the forward pass over the same scores left them:
  *   grad_x_c = grad_logp ([c = target] - p_c) - grad_entropy p_c (x_c - lse + entropy)
+ * p_c = exp(x_c - lse) up to |lse| = 128; above it, where an fp32 lse is too coarse for that, divided by their sum over the classes.
  * Zero at ignored positions (whatever their scores and gradients) and at those with lse = -inf.  A cross entropy's mean over n
  * positions is grad_logp = -1 / n.  grad_logits in the scores' type with rows of its own stride; it may be the scores' own memory
  * if the strides agree.  The elements between two rows are left as they are.

@@ -781,6 +781,11 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void logp_lanes_kernel(const
 }
 
 // ---- gradient -------------------------------------------------------------------------------------------------------------
+// An lse is one fp32 number, and its last bit a factor of every p: up to 2^-24 |lse| of it.  Above LSE_EXACT (2^-17) a row's p are therefore
+// divided by their sum, which costs such a row another pass: by the threads that have it or, where several workgroups do, by one of them
+// alone, so that in place nothing is read that another one has written.  (A forward pass's lse is no less than the largest score: no power
+// overflows.)
+constexpr float LSE_EXACT = 128.f;
 
 struct LogpBwdArgs {
     const int32_t *target;
@@ -791,7 +796,7 @@ struct LogpBwdArgs {
 struct LogpBwdRow {
     int t;
     bool zero;
-    float lse, gl, gh, h;
+    float lse, gl, gh, h, log2_share = 0.f;      // the last: minus log2 of the sum of the p, where they are divided by it
     __device__ __forceinline__ LogpBwdRow(const LogpBwdArgs &a, int64_t row)
     {
         t = a.target ? a.target[row] : -1;
@@ -801,13 +806,58 @@ struct LogpBwdRow {
         gh = a.grad_entropy ? a.grad_entropy[row] : 0.f;
         h = a.grad_entropy ? a.entropy[row] : 0.f;
     }
+    __device__ __forceinline__ bool far() const { return !zero && fabsf(lse) > LSE_EXACT && fabsf(lse) < INFINITY; }
+    __device__ __forceinline__ float term(float x) const { return __builtin_amdgcn_exp2f((x - lse) * LOG2E); }
+    // terms: the sum over all of the row's scores (of an lse that is not the row's own it may be no number to divide by)
+    __device__ __forceinline__ void divide_by(float terms)
+    {
+        if (!(terms > 0.f && terms < INFINITY)) return;
+        log2_share = -log2f(terms);
+        h = __builtin_fmaf(log2_share, LN2, h);
+    }
     __device__ __forceinline__ float operator()(float x, int c) const
     {
-        const float lp = x - lse, p = __builtin_amdgcn_exp2f(lp * LOG2E);
+        const float lp = x - lse, p = __builtin_amdgcn_exp2f(__builtin_fmaf(lp, LOG2E, log2_share));
         const float v = -p * (gl + gh * (fmaxf(lp, MASKED) + h));
         return c == t ? v + gl : v;
     }
 };
+
+// A row by L neighbouring threads, whose elements are a thread's own in both passes.
+template <class T, int L>
+__device__ __forceinline__ void logp_bwd_far_row(const T *at, T *to, int C, LogpBwdRow f)
+{
+    constexpr int N = LANE_ELEMENTS<T>, AHEAD = L == 256 ? 4 : 1;        // (registers of the others are few)
+    const int sub = threadIdx.x % L, pieces = C / N;
+    float terms = 0.f;
+#pragma unroll AHEAD
+    for (int i = sub; i < pieces; i += L) {
+        float v[N];
+        Chunk<T>::load(at + i * N, v);
+#pragma unroll
+        for (int j = 0; j < N; ++j) terms += f.term(v[j]);
+    }
+    for (int c = pieces * N + sub; c < C; c += L) terms += f.term(to_f32(at[c]));
+    terms = lanes_sum<L < 64 ? L : 64>(terms);
+    if (L > 64) {
+        __shared__ float s_terms[L / 64 + 1];
+        if ((threadIdx.x & 63) == 0) s_terms[threadIdx.x >> 6] = terms;
+        __syncthreads();
+        terms = 0.f;
+#pragma unroll
+        for (int i = 0; i < L / 64; ++i) terms += s_terms[i];
+    }
+    f.divide_by(terms);
+#pragma unroll AHEAD
+    for (int i = sub; i < pieces; i += L) {
+        float v[N];
+        Chunk<T>::load(at + i * N, v);
+#pragma unroll
+        for (int j = 0; j < N; ++j) v[j] = f(v[j], i * N + j);
+        Chunk<T>::store(to + i * N, v);
+    }
+    for (int c = pieces * N + sub; c < C; c += L) to[c] = (T)f(to_f32(at[c]), c);
+}
 
 // Point-major: L lanes to a row, U times 16 bytes each, `chunks` workgroups behind one another along long rows (L = 256).  Bound by memory
 // where rows fill their lanes: 336 MB of scores and as much of gradients, bf16, 64 classes 126 us (5.3 TB/s), 100 classes 210, 600 117, 131072
@@ -835,6 +885,14 @@ __global__ __launch_bounds__(256) void logp_bwd_rows_kernel(const T *x, T *gx, L
 #pragma unroll
             for (int j = 0; j < N; ++j)
                 if (c + j < a.C) raw[u][j] = at[c + j];
+    }
+    if (__builtin_expect(f.far(), 0)) {
+        if (L < 256 || blockIdx.x % chunks == row % chunks) logp_bwd_far_row<T, L>(at, to, a.C, f);        // (all the XCDs have some)
+        return;
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        const int c = c0 + u * L * N;
 #pragma unroll
         for (int j = 0; j < N; ++j) v[u][j] = f.zero ? 0.f : f(to_f32(raw[u][j]), c + j);
         Chunk<T>::store_row(to, c, a.C, v[u]);
@@ -851,7 +909,14 @@ __global__ __launch_bounds__(256) void logp_bwd_few_kernel(const T *x, T *gx, Lo
     T *to = gx + row * a.grad_stride;
     float v[R];
     load_few<T, R>(x + row * a.stride, a.C, v);
-    const LogpBwdRow f(a, row);
+    LogpBwdRow f(a, row);
+    if (f.far()) {
+        float terms = 0.f;
+#pragma unroll
+        for (int c = 0; c < R; ++c)
+            if (c < a.C) terms += f.term(v[c]);
+        f.divide_by(terms);
+    }
 #pragma unroll
     for (int q = 0; q < R; q += N) {
         float piece[N];
@@ -878,7 +943,23 @@ __global__ __launch_bounds__(256) void logp_bwd_cols_kernel(const T *x, T *gx, L
     T v[BWD_CLASSES];
 #pragma unroll
     for (int i = 0; i < BWD_CLASSES; ++i) v[i] = at[min(i, many - 1) * a.stride];        // (in no branch: all before the first is converted)
-    const LogpBwdRow f(a, b * a.N + n);
+    LogpBwdRow f(a, b * a.N + n);
+    if (f.far()) {        // one part's lane takes all of the position's classes
+        if (part != tile % parts) return;
+        at -= first * a.stride;
+        to -= first * a.grad_stride;
+        float terms = 0.f;
+        for (int c = 0; c < a.C; c += BWD_CLASSES) {
+            float some = 0.f;
+#pragma unroll 4
+            for (int i = c; i < min(c + BWD_CLASSES, a.C); ++i) some += f.term(to_f32(at[i * a.stride]));
+            terms += some;
+        }
+        f.divide_by(terms);
+#pragma unroll 4
+        for (int c = 0; c < a.C; ++c) to[c * a.grad_stride] = (T)f(to_f32(at[c * a.stride]), c);
+        return;
+    }
 #pragma unroll
     for (int i = 0; i < BWD_CLASSES; ++i)
         if (i < many) to[i * a.grad_stride] = (T)(f.zero ? 0.f : f(to_f32(v[i]), first + i));

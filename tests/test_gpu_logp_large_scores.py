@@ -6,7 +6,7 @@ import torch
 
 import paper_1803_07289_amd as fx
 from gpu_util import say
-from operator_util import TYPES, U, chain, laid_out, to_positions, within
+from operator_util import TYPES, U, chain, half_step, laid_out, smallest_half, to_positions, within
 
 pytestmark = pytest.mark.gpu
 
@@ -125,3 +125,40 @@ def test_a_shift_of_all_scores_changes_nothing(C, layout):
         assert float((got[1] - base[1]).abs().max()) <= 4 * k * (1 + float(base[1].abs().max()))
         assert float((got[3] - base[3]).abs().max()) <= 2 * k + 2 * U * float(base[3].abs().max())
         assert torch.equal(got[4], base[4])
+
+
+def check_bwd(x, t, h, gl, gh, got, dtype, layout):
+    """From p as it is, not from an lse rounded to fp32."""
+    m = x.max(1)
+    z = x - m[:, None]
+    with np.errstate(all="ignore"):
+        log_s = np.log(np.exp(z).sum(1))
+        lp = z - log_s[:, None]
+        p = np.exp(lp)
+        lp = np.where(np.isneginf(lp), 0.0, lp)
+    want = -gh[:, None] * p * (lp + h[:, None]) - gl[:, None] * p
+    want[np.arange(len(x)), t] += gl
+    part = np.abs(gl)[:, None] + np.abs(gh)[:, None] * (np.abs(lp) + np.abs(h)[:, None] + 1)
+    # the exponent's roundings 3 U |lp|, the power's 2 U, those of the products; half a step of an lse up to 128, or those of a sum
+    off = (3 * np.abs(lp) + 10 + np.minimum(np.abs(m + log_s), 128)[:, None]) * U + chain(x.shape[1], 64)
+    within(to_positions(got, layout), want, p * part * off + 2 * U * np.abs(gl)[:, None] + half_step(dtype) * np.abs(want) +
+           smallest_half(dtype), "grad_logits")
+
+
+@pytest.mark.parametrize("layout", [fx.BNC, fx.BCN], ids=["bnc", "bcn"])
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("C", [6, 13, 20, 40, 100, 300, 700, 1500, 2500, 9001, 70000])
+def test_gradients_of_scores_of_any_size(C, dtype, layout):
+    say(f"logp large scores, gradient {C} {dtype} {layout}")
+    td = TYPES[dtype]
+    x, t = rows_of_all_sizes(C, td)
+    rng = np.random.default_rng(C + 5)
+    gl, gh = (rng.standard_normal(len(x)).astype(np.float32) for _ in range(2))
+    d = lambda a: torch.from_numpy(a)[None].cuda()
+    dx, dt = laid_out(x, 1, layout, td, 1, (len(x) if layout == fx.BCN else C) + 3), d(t.astype(np.int32))
+    _, h, lse, _, _ = fx.flexlogp_fwd(dx, dt, layout=layout)
+    hh = h.double().cpu().numpy().reshape(-1)
+    got = fx.flexlogp_bwd(dx, dt, lse, h, d(gl), d(gh), layout=layout)
+    check_bwd(x, t, hh, gl, gh, got, td, layout)
+    back = fx.flexlogp_bwd(dx, dt, lse, None, d(gl), layout=layout, out=dx)           # in place
+    check_bwd(x, t, hh, gl, np.zeros_like(gh), back, td, layout)
