@@ -6,8 +6,9 @@
 // never move it: states are rounded at random, with probabilities that make the mean exact.  v is kept by its root, which spreads
 // its range over twice the exponents; the choice between two roots is made so that the square has the right mean, and a v
 // above zero is never stored as zero, which would leave eps alone under m.  The random bits are a hash of (seed, step,
-// tensor, element).  What leads to a state is rounded operation by operation (no fused multiply-adds but where they are exact), so
-// that states are the same bits wherever the formulas are evaluated in fp32.
+// tensor, element).  What leads to a state is rounded operation by operation (no fused multiply-adds but where they are exact), a block's
+// exponent comes from a correctly rounded root, and a code hardly depends on its root's last bit (see second_code): states are the same
+// bits wherever the formulas are evaluated in fp32, but for a random number of 0 within an ulp of a code's border.
 #include "flex_elem.hpp"
 #include <algorithm>
 #include <math.h>
@@ -134,7 +135,8 @@ __device__ __forceinline__ uint32_t first_code(float value, uint32_t r, uint32_t
     return (uint32_t)__builtin_amdgcn_cvt_sr_fp8_f32(value, (int)r, (int)word, i);
 }
 // The state of a second moment v, its root and the scale of its block: in steps of e4m3 at the root's exponent, n below it and n + 1 above
-// it, their squares n^2 and n^2 + 2 n + 1; up where the random share of the difference lies below v.
+// it, their squares n^2 and n^2 + 2 n + 1; up where the random share of the difference lies below v.  (A root that is an ulp too small or
+// too large at n's border makes n one less or more, and `up` always or never true: the same code.)
 __device__ __forceinline__ uint32_t second_code(float v, float root, float down, uint32_t r16)
 {
     const float y = root * down;
@@ -143,7 +145,7 @@ __device__ __forceinline__ uint32_t second_code(float v, float root, float down,
     const float n = floorf(y * f), w = v * f2 * f2;
     const bool up = (float)r16 * __builtin_fmaf(n, 0x1p-15f, 0x1p-16f) < __builtin_fmaf(-n, n, w);              // (both products exact)
     const int code = (int)((power >> 20) + (uint32_t)n) - 968 + (up ? 1 : 0);
-    return (uint32_t)min(max(code, (int)min(bits, 1u)), 126);       // (the largest finite one; above zero, not zero)
+    return (uint32_t)min(max(code, (int)min(__builtin_bit_cast(uint32_t, v), 1u)), 126);       // (the largest finite one; above zero, not zero)
 }
 
 __device__ __forceinline__ void store_codes(uint8_t *codes, uint8_t *scale, const uint32_t (&word)[2], int e, int64_t at, int64_t count)
@@ -209,6 +211,11 @@ __device__ __forceinline__ void store8(T *p, const float (&x)[8], int64_t at, in
 // four lanes.  Memory bounds it: 5.4 TB/s with states in 32 bits and a copy (28 bytes an element, 191M elements: 997 us; at the rate of a copy 869),
 // 5.7 with states in 8 (10.1 bytes, 428M elements in bf16: 765 us, 704), where the vector unit has some 60 operations an element to hide.  Larger
 // pieces, two pieces a workgroup and accesses past the caches measured the same or worse.
+// Roots and quotients are the hardware's approximations, an ulp each: the update is lr times them, an ulp of it no ulp of p.  Of a
+// subnormal v the hardware's root is 0; that is told from eps, or in a state of 8 bits from the values beside it, only below the two bounds
+// here, and there the root is the full one.
+constexpr float ROOT_BESIDE_EPS = 0x1p-38f;         // 2^-63 of a subnormal's root is 2^-25 of it
+constexpr float BLOCK_OF_SUBNORMALS = 0x1p-88f;     // the largest v whose block has codes for the root of a subnormal one: 448^2 2^18 2^-126 at most
 template <class P, class G, int BITS>
 __global__ __launch_bounds__(256) void adamw_step_kernel(AdamwPlan plan, int copy_dtype)
 {
@@ -219,7 +226,7 @@ __global__ __launch_bounds__(256) void adamw_step_kernel(AdamwPlan plan, int cop
     const G *grad = (const G *)plan.grads[k];
     if (!grad) return;                       // a tensor without a gradient keeps its values and states
     const int64_t at = (int64_t)(blockIdx.x - t.first) * ADAMW_CHUNK + threadIdx.x * 8;
-    float p[8], g[8], m[8], v[8], root[8];
+    float p[8], g[8], m[8], v[8], root[8], largest_v = 0.f;
     load8((const P *)t.p, p, at, t.count);
     load8(grad, g, at, t.count);
     if (BITS == 32) {
@@ -237,8 +244,20 @@ __global__ __launch_bounds__(256) void adamw_step_kernel(AdamwPlan plan, int cop
         g[i] *= h.grad_scale;
         m[i] = m[i] * h.b1 + g[i] * h.a1;
         v[i] = v[i] * h.b2 + g[i] * g[i] * h.a2;
-        // root and quotient by the hardware's approximations, an ulp each: the update is lr times them, an ulp of it no ulp of p
-        root[i] = __builtin_amdgcn_sqrtf(v[i]);
+    }
+    bool full_roots = h.eps < h.rsqrt_c2 * ROOT_BESIDE_EPS;
+    if (BITS == 8) {
+        largest_v = block_max(v);
+        full_roots |= __any(largest_v > 0.f && largest_v < BLOCK_OF_SUBNORMALS);
+    }
+    if (__builtin_expect(full_roots, 0))
+#pragma unroll
+        for (int i = 0; i < 8; ++i) root[i] = sqrtf(v[i]);
+    else
+#pragma unroll
+        for (int i = 0; i < 8; ++i) root[i] = __builtin_amdgcn_sqrtf(v[i]);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
         const float by = m[i] * __builtin_amdgcn_rcpf(__builtin_fmaf(root[i], h.rsqrt_c2, h.eps));
         p[i] = __builtin_fmaf(-by, h.step_size, p[i] * keep);
     }
@@ -253,7 +272,7 @@ __global__ __launch_bounds__(256) void adamw_step_kernel(AdamwPlan plan, int cop
         return;
     }
     const uint32_t key = adamw_mix(h.key + k);
-    const int em = block_exponent(block_max(m)), ev = block_exponent(block_max(root));
+    const int em = block_exponent(block_max(m)), ev = block_exponent(sqrtf(largest_v));
     const float down_m = power2(-em), down_v = power2(-ev);
     uint32_t cm[2] = {0, 0}, cv[2] = {0, 0};
 #pragma unroll

@@ -11,6 +11,7 @@ from operator_util import TYPES, U, half_step, smallest_half, within
 pytestmark = pytest.mark.gpu
 
 SIZES = [1, 7, 8, 31, 32, 33, 100, 0, 2047, 2048, 2049, 4096, 5000, 65537]
+F32 = np.float32
 LR, BETAS, EPS = 0.01, (0.9, 0.99), 1e-6
 
 
@@ -139,6 +140,49 @@ def test_a_long_run_in_8_bits_follows_one_in_32():
     # 0.3 / sqrt(1 - beta2^2) / sqrt(n) = 0.012 of the value; five of them
     assert abs(float(v8.mean() / v1.mean()) - 1) < 0.06
     assert abs(float(m8.mean() / m1.mean()) - 1) < 0.06
+
+
+@pytest.mark.parametrize("size", [1e-18, 1e-20, 1e-21])
+@pytest.mark.parametrize("eps", [1e-8, 1e-13, 1e-25, 1e-36])
+def test_second_moments_of_the_smallest_gradients(size, eps):
+    """v = 0.01 g^2 below fp32's normal numbers: its root stands above eps all the same."""
+    n = 5000
+    rng = np.random.default_rng(6)
+    g = torch.from_numpy(rng.choice([-1.0, 1.0], n) * (1 + rng.random(n)) * size).float().cuda()
+    p = torch.zeros(n, device="cuda")
+    m, v, _, _ = fx.flexadamw_state([p])
+    plan = fx.flexadamw_plan_build([p], m, v, betas=BETAS, eps=eps)
+    fx.flexadamw_step(plan, [g], LR)
+    m, v = m[0].double().cpu().numpy(), v[0].double().cpu().numpy()
+    assert np.all(v > 0)
+    # from the moments as they were stored: root, correction, sum, quotient, two products, of an ulp (2 U) each at most
+    want = -LR * (m / (1 - BETAS[0])) / (np.sqrt(v / (1 - BETAS[1])) + eps)
+    within(p.double().cpu().numpy(), want, 12 * U * np.abs(want) + 2.0 ** -149, "p")
+
+
+@pytest.mark.parametrize("eps", [1e-6, 1e-30])
+def test_8_bit_states_of_the_smallest_gradients(eps):
+    """Second moments below fp32's normal numbers, in blocks of their own and beside large ones: above zero they are stored above zero."""
+    n = 4096
+    rng = np.random.default_rng(7)
+    g = (rng.choice([-1.0, 1.0], n) * 10.0 ** -(17 + 4.2 * rng.random(n))).astype(np.float32)
+    g[:1024:32] = 0.5                                                  # (the first blocks have a large one each)
+    g[1024:2048] = (g[1024:2048].astype(np.float64) * 1e4).astype(np.float32)
+    g[::7] = 0
+    p = torch.zeros(n, device="cuda")
+    m, v, ms, vs = fx.flexadamw_state([p], 8)
+    plan = fx.flexadamw_plan_build([p], m, v, ms, vs, betas=BETAS, eps=eps, seed=9)
+    for t in (1, 2):
+        was = [codes_of(x)[0] for x in (m, ms, v, vs)]
+        before = p.cpu().numpy()
+        fx.flexadamw_step(plan, [torch.from_numpy(g).cuda()], LR)
+        want_p, *want = ref.adamw_8bit(before, *was, g, t, LR, *BETAS, eps, 0.0, 9, 0)
+        for got, w, name in zip((codes_of(x)[0] for x in (m, ms, v, vs)), want, ("m", "m scale", "v", "v scale")):
+            assert np.array_equal(got, w), (name, t, int(np.sum(got != w)))
+        live = (F32(1 - BETAS[1]) * g * g) > 0
+        assert np.all(codes_of(v)[0][live] > 0)
+        # the formula in fp32, a handful of roundings on either side
+        within(p.double().cpu().numpy(), want_p, 24 * U * np.maximum(np.abs(want_p), np.abs(want_p - before)) + 4 * U * np.abs(before), "p")
 
 
 def test_no_gradient_and_no_step():
