@@ -419,7 +419,7 @@ typedef enum { FLEX_F32 = 0, FLEX_BF16 = 1, FLEX_F16 = 2 } flex_dtype;
  * Layer norm over the C channels of every position:
  *   y = (x - mean) * rstd * weight + bias,  mean over the channels,  rstd = 1 / sqrt(mean((x - mean)^2) + eps)
  * weight / bias [C] in param_dtype (FLEX_F32 or x's type); both NULL: not scaled.  mean / rstd fp32 [B,N] for the backward pass;
- * either may be NULL.  y must not overlap x (y == x is refused).  eps >= 0, C <= FLEX_NORM_MAX_CHANNELS.
+ * either may be NULL.  A y that shares memory with x is refused.  eps >= 0, C <= FLEX_NORM_MAX_CHANNELS.
  */
 #define FLEX_NORM_MAX_CHANNELS (1 << 20)
 int flexnorm_fwd(const void *x, const void *weight, const void *bias, void *y, float *mean, float *rstd,
@@ -467,7 +467,7 @@ int flexlogp_fwd(const void *logits, const int32_t *target, float *logp, float *
  * p_c = exp(x_c - lse) up to |lse| = 128; above it, where an fp32 lse is too coarse for that, divided by their sum over the classes.
  * Zero at ignored positions (whatever their scores and gradients) and at those with lse = -inf.  A cross entropy's mean over n
  * positions is grad_logp = -1 / n.  grad_logits in the scores' type with rows of its own stride; it may be the scores' own memory
- * if the strides agree.  The elements between two rows are left as they are.
+ * if the strides agree, or lie between their rows; rows that share memory with others are refused.  The elements between two rows are left as they are.
  */
 int flexlogp_bwd(const void *logits, const int32_t *target, const float *lse, const float *entropy,
                  const float *grad_logp, const float *grad_entropy, void *grad_logits, int B, int N, int C,
@@ -487,7 +487,8 @@ int flexlogp_bwd(const void *logits, const int32_t *target, const float *lse, co
  *             that its mean is exact (v in the square), by bits that depend on (seed, step, tensor, element) alone; a v above
  *             zero is never stored as zero.  All zero bytes are the state before the first step.
  *   copy      copy_dtype (FLEX_BF16 / FLEX_F16), or NULL: the new values once more, for a network that computes in 16 bits
- * flexadamw_step: grads host array of n device pointers, all of grad_dtype; NULL: that tensor is left as it is.  lr, or *lr_dev
+ * flexadamw_step: grads host array of n device pointers, all of grad_dtype, in memory that none of the list's tensors is in; NULL: that
+ * tensor is left as it is.  lr, or *lr_dev
  * where lr_dev (device) is not NULL; grad_scale device, or NULL for 1.  A grad_scale that is not finite: nothing is changed and
  * the step is not counted (a loss scale that overflowed, decided on the device).  Gradients must be finite otherwise.
  */

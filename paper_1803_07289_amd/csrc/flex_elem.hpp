@@ -3,6 +3,7 @@
 #pragma once
 #include "flex_common.hpp"
 #include "../../include/flexconv.h"
+#include <algorithm>
 #include <type_traits>
 
 namespace flex {
@@ -16,6 +17,22 @@ static inline bool dtype_ok(int d) { return d == FLEX_F32 || d == FLEX_BF16 || d
 static inline size_t dtype_bytes(int d) { return d == FLEX_F32 ? 4 : 2; }
 // Positions of a call: those of a last workgroup that lies past the end are numbered in an int too.
 static inline bool positions_ok(int B, int N) { return B > 0 && N > 0 && (int64_t)B * N <= INT32_MAX - 1023; }
+// Whether two sets of `rows` rows of `width` bytes, which lie sa and sb bytes apart, share memory.
+static inline bool rows_share(const void *a, int64_t sa, const void *b, int64_t sb, int64_t rows, int64_t width)
+{
+    const int64_t d = (int64_t)((uintptr_t)b - (uintptr_t)a);
+    if (d >= (rows - 1) * sa + width || -d >= (rows - 1) * sb + width) return false;
+    if (sa == sb) {        // halves of wider rows, say: their places within a row decide
+        const int64_t place = ((d % sa) + sa) % sa;
+        return place < width || place > sa - width;
+    }
+    for (int64_t i = 0; i < rows; ++i) {        // the rows of b around the place of a's row i: the first that ends behind its begin
+        const int64_t j = std::max<int64_t>(0, (i * sa - d - width) / sb);
+        for (int64_t k = j; k < std::min(rows, j + 3); ++k)
+            if (d + k * sb < i * sa + width && i * sa < d + k * sb + width) return true;
+    }
+    return false;
+}
 // A launch counts its threads in 32 bits.
 static inline bool one_launch(int64_t threads) { return threads < (int64_t)1 << 32; }
 

@@ -1168,8 +1168,11 @@ int flexlogp_bwd(const void *logits, const int32_t *target, const float *lse, co
     if (!logits || !lse || !grad_logits || (!grad_logp && !grad_entropy) || (grad_logp && !target) || (grad_entropy && !entropy))
         return FLEX_ERR_NULL;
     if (!logp_sizes_ok(B, N, C, row_stride, dtype, layout) || !logp_sizes_ok(B, N, C, grad_row_stride, dtype, layout)) return FLEX_ERR_SHAPE;
-    if (logits == grad_logits && row_stride != grad_row_stride) return FLEX_ERR_SHAPE;
     const bool bcn = layout == FLEX_LAYOUT_BCN;
+    const int64_t e_bytes = (int64_t)dtype_bytes(dtype);
+    if (!(logits == grad_logits && row_stride == grad_row_stride) &&
+        rows_share(logits, row_stride * e_bytes, grad_logits, grad_row_stride * e_bytes, (int64_t)B * (bcn ? C : N), (bcn ? N : C) * e_bytes))
+        return FLEX_ERR_SHAPE;
     const LogpBwdArgs a{target, lse, entropy, grad_logp, grad_entropy, (int64_t)B * N, row_stride, grad_row_stride, N, C};
     const hipError_t e = with_dtype(dtype, [&](auto t) {
         typedef decltype(t) T;

@@ -1051,6 +1051,11 @@ static bool norm_sizes_ok(int B, int N, int C, int layout, int dtype, int param_
            dtype_ok(dtype) && (param_dtype == FLEX_F32 || param_dtype == dtype) &&
            one_launch(norm_threads(B, N, C, dtype, layout == FLEX_LAYOUT_BCN));
 }
+static bool norm_tensors_share(const void *a, const void *b, int B, int N, int C, int dtype)
+{
+    const int64_t bytes = (int64_t)B * N * C * (int64_t)dtype_bytes(dtype);
+    return rows_share(a, bytes, b, bytes, 1, bytes);
+}
 
 extern "C" {
 
@@ -1058,7 +1063,7 @@ int flexnorm_fwd(const void *x, const void *weight, const void *bias, void *y, f
                  float eps, int dtype, int param_dtype, int layout, void *stream)
 {
     if (!x || !y || (weight == nullptr) != (bias == nullptr)) return FLEX_ERR_NULL;
-    if (!norm_sizes_ok(B, N, C, layout, dtype, param_dtype) || !(eps >= 0.f) || x == y) return FLEX_ERR_SHAPE;
+    if (!norm_sizes_ok(B, N, C, layout, dtype, param_dtype) || !(eps >= 0.f) || norm_tensors_share(x, y, B, N, C, dtype)) return FLEX_ERR_SHAPE;
     const hipError_t e = with_dtype(dtype, [&](auto t) {
         typedef decltype(t) T;
         return launch_norm_fwd<T>((const T *)x, weight, bias, (T *)y, mean, rstd, B, N, C, eps, param_dtype, layout == FLEX_LAYOUT_BCN,
@@ -1079,7 +1084,8 @@ int flexnorm_bwd(const void *x, const void *weight, const void *grad_out, const 
 {
     if (!x || !grad_out || !mean || !rstd || (grad_weight == nullptr) != (grad_bias == nullptr) || (!grad_x && !grad_weight))
         return FLEX_ERR_NULL;
-    if (!norm_sizes_ok(B, N, C, layout, dtype, param_dtype) || grad_x == x || grad_x == grad_out) return FLEX_ERR_SHAPE;
+    if (!norm_sizes_ok(B, N, C, layout, dtype, param_dtype) ||
+        (grad_x && (norm_tensors_share(x, grad_x, B, N, C, dtype) || norm_tensors_share(grad_out, grad_x, B, N, C, dtype)))) return FLEX_ERR_SHAPE;
     if (grad_weight && (!workspace || ((uintptr_t)workspace & 255) || workspace_bytes < flexnorm_bwd_workspace_bytes(B, N, C, dtype, layout)))
         return FLEX_ERR_WORKSPACE;
     const hipError_t e = with_dtype(dtype, [&](auto t) {

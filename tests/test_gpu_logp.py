@@ -240,3 +240,25 @@ def test_refusals_of_the_binding():
                         (g(x, t, lse, h, lse, out=x.half()), ValueError)):
         with pytest.raises(error):
             call()
+
+
+@pytest.mark.parametrize("layout", [fx.BNC, fx.BCN], ids=["bnc", "bcn"])
+def test_a_gradient_between_the_rows_of_its_scores(layout):
+    """Both in one buffer, rows of one between rows of the other: taken; an element closer: refused before anything is written."""
+    _, x = scores(3, 60, 13, torch.float32)
+    width = 30 if layout == fx.BCN else 13
+    wide = torch.full((2, 13, 64) if layout == fx.BCN else (2, 30, 29), 7.0, device="cuda")
+    view, out = wide[:, :, :width], wide[:, :, width:2 * width]
+    view.copy_(laid_out(x, 2, layout, torch.float32))
+    t = torch.zeros(2, 30, dtype=torch.int32, device="cuda")
+    _, h, lse, _, _ = fx.flexlogp_fwd(view, t, layout=layout)
+    before = wide.clone()
+    with pytest.raises(fx.FlexError):
+        fx.flexlogp_bwd(view, t, lse, None, torch.ones_like(lse), layout=layout, out=wide[:, :, width - 1:2 * width - 1])
+    assert torch.equal(wide, before)
+    fx.flexlogp_bwd(view, t, lse, None, torch.ones_like(lse), layout=layout, out=out)
+    check_bwd(x, np.zeros(60, int), lse.double().cpu().numpy().reshape(-1), None, np.ones(60), None, out, torch.float32, layout)
+    assert torch.equal(view, before[:, :, :width]) and bool((wide[:, :, 2 * width:] == 7).all())
+    flat = torch.zeros(64 * 6 + 8, device="cuda")
+    with pytest.raises(fx.FlexError):
+        fx.flexnorm_fwd(flat[:384].view(2, 6, 32), layout=layout, out=flat[8:392].view(2, 6, 32))

@@ -152,3 +152,38 @@ def test_the_binding_refuses_tensors_of_the_cpu():
         fx.flexadamw_plan_build([x], [], [x])
     with pytest.raises(ValueError):
         fx.flexadamw_state([x], bits=16)
+
+
+def at(address):
+    return ctypes.c_void_p(address)
+
+
+@pytest.mark.parametrize("layout", [0, 1])
+@pytest.mark.parametrize("dtype, size", [(0, 4), (1, 2), (2, 2)])
+def test_norm_refuses_results_that_share_memory_with_its_inputs(L, dtype, size, layout):
+    """Tensors of 8 positions of 4 channels, an element, a position or all but an element apart, either way round."""
+    x = 1 << 20
+    for d in (size, 4 * size, 31 * size, 1, 32 * size - 1):
+        for y in (x - d, x + d):
+            assert norm_fwd(L, x=at(x), y=at(y), dtype=dtype, pdtype=dtype, layout=layout) == 2
+            assert norm_bwd(L, x=at(x), g=at(2 * x), gx=at(y), dtype=dtype, pdtype=dtype, layout=layout) == 2
+            assert norm_bwd(L, x=at(2 * x), g=at(x), gx=at(y), dtype=dtype, pdtype=dtype, layout=layout) == 2
+
+
+@pytest.mark.parametrize("layout", [0, 1])
+@pytest.mark.parametrize("dtype, size", [(0, 4), (1, 2), (2, 2)])
+def test_gradient_of_the_scores_refuses_rows_that_share_memory_with_others(L, dtype, size, layout):
+    x, (N, C) = 1 << 20, (5, 7)
+    rows, width = (7, 5) if layout == 0 else (5, 7)
+    f = lambda gx, row, grow: logp_bwd(L, x=at(x), gx=at(gx), N=N, C=C, row=row, grow=grow, dtype=dtype, layout=layout)
+    cases = [(d, row, row) for row in (width, 20) for d in (1, -1, width - 1, 1 - width, row + 1, row - 1, (rows - 1) * row + width - 1)]
+    cases += [(d, row, grow) for row, grow in ((8, 16), (24, 16), (9, 7), (16, 41)) for d in (0, 1, -1, 2 * row)]
+    held = 0
+    for d, row, grow in cases:
+        a = {i * row + j for i in range(rows) for j in range(width)}
+        b = {d + i * grow + j for i in range(rows) for j in range(width)}
+        if a & b:
+            held += 1
+            assert f(x + d * size, row, grow) == 2, (d, row, grow)
+    assert held > 25
+    assert f(x, 20, 21) == 2 and f(x + 1, width, width) == 2 and f(x - 1, width, width) == 2
