@@ -7,7 +7,7 @@
 // its range over twice the exponents; the choice between two roots is made so that the square has the right mean, and a v
 // above zero is never stored as zero, which would leave eps alone under m.  The random bits are a hash of (seed, step,
 // tensor, element).  What leads to a state is rounded operation by operation (no fused multiply-adds but where they are exact), a block's
-// exponent comes from a correctly rounded root, and a code hardly depends on its root's last bit (see second_code): states are the same
+// exponent is that of a correctly rounded root, and a code hardly depends on its root's last bit (see second_code): states are the same
 // bits wherever the formulas are evaluated in fp32, but for a random number of 0 within an ulp of a code's border.
 #include "flex_elem.hpp"
 #include <algorithm>
@@ -127,6 +127,14 @@ __device__ __forceinline__ int block_exponent(float largest)
     return min(max(e, -100), 120);
 }
 
+// The same of the root of a normal v: half of v's exponent, and one more where the root is above 1.75 times a power of two, that is v above
+// 3.0625 times its square (its rounded root is, exactly then).
+__device__ __forceinline__ int root_exponent(float v)
+{
+    const uint32_t bits = __builtin_bit_cast(uint32_t, v);
+    return (int)(((bits >> 23) + 1) >> 1) - 72 + ((bits & 0xFFFFFFu) - 0x440001u < 0x3BFFFFu);
+}
+
 // The state that lies up or down from `value` (a first moment times its block's scale) by 16 random bits in the upper half of r: the
 // hardware's conversion, which adds them below the last bit kept, subnormals too.  Into byte i of word.
 template <int i>
@@ -226,7 +234,7 @@ __global__ __launch_bounds__(256) void adamw_step_kernel(AdamwPlan plan, int cop
     const G *grad = (const G *)plan.grads[k];
     if (!grad) return;                       // a tensor without a gradient keeps its values and states
     const int64_t at = (int64_t)(blockIdx.x - t.first) * ADAMW_CHUNK + threadIdx.x * 8;
-    float p[8], g[8], m[8], v[8], root[8], largest_v = 0.f;
+    float p[8], g[8], m[8], v[8], root[8];
     load8((const P *)t.p, p, at, t.count);
     load8(grad, g, at, t.count);
     if (BITS == 32) {
@@ -246,9 +254,11 @@ __global__ __launch_bounds__(256) void adamw_step_kernel(AdamwPlan plan, int cop
         v[i] = v[i] * h.b2 + g[i] * g[i] * h.a2;
     }
     bool full_roots = h.eps < h.rsqrt_c2 * ROOT_BESIDE_EPS;
+    int ev = 0;
     if (BITS == 8) {
-        largest_v = block_max(v);
-        full_roots |= __any(largest_v > 0.f && largest_v < BLOCK_OF_SUBNORMALS);
+        const float largest = block_max(v);
+        full_roots |= __any(largest > 0.f && largest < BLOCK_OF_SUBNORMALS);
+        ev = full_roots ? block_exponent(sqrtf(largest)) : largest > 0.f ? root_exponent(largest) : block_exponent(0.f);
     }
     if (__builtin_expect(full_roots, 0))
 #pragma unroll
@@ -272,7 +282,7 @@ __global__ __launch_bounds__(256) void adamw_step_kernel(AdamwPlan plan, int cop
         return;
     }
     const uint32_t key = adamw_mix(h.key + k);
-    const int em = block_exponent(block_max(m)), ev = block_exponent(sqrtf(largest_v));
+    const int em = block_exponent(block_max(m));
     const float down_m = power2(-em), down_v = power2(-ev);
     uint32_t cm[2] = {0, 0}, cv[2] = {0, 0};
 #pragma unroll

@@ -185,6 +185,26 @@ def test_8_bit_states_of_the_smallest_gradients(eps):
         within(p.double().cpu().numpy(), want_p, 24 * U * np.maximum(np.abs(want_p), np.abs(want_p - before)) + 4 * U * np.abs(before), "p")
 
 
+def test_exponents_of_blocks_at_their_borders():
+    """Blocks of one value each, whose second moments step through the places where the root's exponent changes."""
+    a2 = F32(1 - BETAS[1])
+    g = []
+    for k in range(-30, 30, 3):
+        for square in (3.0625, 1.0):
+            x = F32(np.sqrt(square * 2.0 ** (2 * k) / a2))
+            g.append((x.view(np.int32) + np.arange(-40, 41, dtype=np.int32)).view(F32))
+    g = np.repeat(np.concatenate(g), 32)
+    p = torch.zeros(len(g), device="cuda")
+    m, v, ms, vs = fx.flexadamw_state([p], 8)
+    plan = fx.flexadamw_plan_build([p], m, v, ms, vs, betas=BETAS, eps=EPS, seed=3)
+    was = [codes_of(x)[0] for x in (m, ms, v, vs)]
+    _, *want = ref.adamw_8bit(p.cpu().numpy(), *was, g, 1, LR, *BETAS, EPS, 0.0, 3, 0)
+    assert len(np.unique(want[3])) >= 40
+    fx.flexadamw_step(plan, [torch.from_numpy(g).cuda()], LR)
+    for got, w, name in zip((codes_of(x)[0] for x in (m, ms, v, vs)), want, ("m", "m scale", "v", "v scale")):
+        assert np.array_equal(got, w), (name, int(np.sum(got != w)))
+
+
 def test_no_gradient_and_no_step():
     _, params = tensors(3, [100, 3000, 50], torch.float32)
     m, v, ms, vs = fx.flexadamw_state(params, 8)
