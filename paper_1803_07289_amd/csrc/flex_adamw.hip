@@ -216,8 +216,8 @@ __device__ __forceinline__ void store8(T *p, const float (&x)[8], int64_t at, in
 }
 
 // A workgroup to 2048 elements of a tensor, eight to a thread, which makes every access 16 or 8 bytes a lane and a scale's 32 elements
-// four lanes.  Memory bounds it: 5.4 TB/s with states in 32 bits and a copy (28 bytes an element, 191M elements: 997 us; at the rate of a copy 869),
-// 5.7 with states in 8 (10.1 bytes, 428M elements in bf16: 765 us, 704), where the vector unit has some 60 operations an element to hide.  Larger
+// four lanes.  Memory bounds it: 5.4 TB/s with states in 32 bits and a copy (28 bytes an element, 191M elements: 998 us; at the rate of a copy 869),
+// 5.6 with states in 8 (10.1 bytes, 428M elements in bf16: 775 us, 704), where the vector unit has some 60 operations an element to hide.  Larger
 // pieces, two pieces a workgroup and accesses past the caches measured the same or worse.
 // Roots and quotients are the hardware's approximations, an ulp each: the update is lr times them, an ulp of it no ulp of p.  Of a
 // subnormal v the hardware's root is 0; that is told from eps, or in a state of 8 bits from the values beside it, only below the two bounds

@@ -202,9 +202,9 @@ __device__ __forceinline__ void lds_in_order()
 // the only ones that are looked at where a row has 32 lanes or more, and so on for each alternative.  Where a row has the wave to itself and more
 // than four are asked for, what reaches the `top`-th largest of the lanes' maxima is listed and ranked, in the time of six.
 // Scores of 16 bits go into one number with their classes, for which an element costs two operations instead of five.
-// us for 336 MB of scores, 0, 1 and 20 alternatives: bf16, 64 classes 81, 95 and 330, 256 classes 71, 84 and 286, 300 classes 83, 103 and 384,
-// 1500 classes 79, 94 and 132 (by the longer rows' workgroups 291, 467 and 550), 4096 classes 84, 103 and 135 (118, 173 and 209);
-// fp32, 64 classes 64, 67 and 242, 600 classes 66, 73 and 119 (241, 413 and 473), 2048 classes 56, 58 and 88 (79, 131 and 151).
+// us for 336 MB of scores, 0, 1 and 20 alternatives: bf16, 64 classes 67, 88 and 325, 256 classes 66, 82 and 285, 300 classes 73, 97 and 382,
+// 1500 classes 68, 89 and 123 (by the longer rows' workgroups 291, 467 and 550), 4096 classes 77, 98 and 128 (118, 173 and 209);
+// fp32, 64 classes 61, 65 and 232, 700 classes 55, 58 and 97 (600 classes 241, 413 and 473), 2048 classes 54, 56 and 82 (79, 131 and 151).
 constexpr int ROW_LIST = 96;
 template <class T, int L, int U>
 __global__ __launch_bounds__(256) void logp_rows_kernel(const T *__restrict__ x, LogpArgs a)
@@ -379,9 +379,9 @@ __global__ __launch_bounds__(256) void logp_rows_kernel(const T *__restrict__ x,
 // and an older one is a lower bound too.  A list that fills up (rows of equal scores, ascending rows) is cut to the best `top`;
 // scores of later spans then have to exceed the last of them.  The lists meet in one, cut by the largest bound of the four waves,
 // and are ranked there.  Parts of one row meet in logp_join_kernel.
-// 2046 x 129280 bf16, a tenth ignored, 8 alternatives: 89 us (476 MB, 5.3 TB/s).  One row of 131072 bf16, 20 alternatives: 6 us in 16 parts
-// and 4.5 to join them.  336 MB of scores, 0, 1 and 20 alternatives: bf16, 5000 classes 95, 143 and 176 us (a span is 8192), 131072 classes
-// 55, 59 and 72; fp32, 4096 classes 49, 70 and 83, 131072 classes 55, 59 and 71.
+// 2046 x 129280 bf16, a tenth ignored, 8 alternatives: 91 us (476 MB, 5.2 TB/s).  One row of 131072 bf16, 20 alternatives: 6 us in 16 parts
+// and 4.5 to join them.  336 MB of scores, 0, 1 and 20 alternatives: bf16, 5000 classes 93, 143 and 174 us (a span is 8192), 131072 classes
+// 55, 58 and 73; fp32, 4096 classes 49, 66 and 83, 131072 classes 53, 59 and 67.
 template <class T>
 __global__ __launch_bounds__(256) void logp_part_kernel(const T *__restrict__ x, LogpArgs a, LogpParts p)
 {
@@ -634,8 +634,10 @@ __device__ __forceinline__ void load_few(const T *row, int C, float (&v)[R])
 // for each alternative.  What the waves find meets in LDS.
 // ROWS: point-major; the lanes of a wave read their rows 16 bytes at a time, which fills whole lines over a few loads.
 // 1M x 13 fp32 with 3 alternatives, point-major: 18.9 us, 92 MB (without alternatives 13.6, 68 MB); channel-major 20 (13.9).  A wave's
-// stores decide beside the memory: those of a row's alternatives, 4 bytes at a time, made it 21.6.  Channel-major, 168 MB of scores: fp32,
-// 16 classes 42 us, 64 39, 256 57, 400 67; bf16, 16 classes 55 (113 when each load was converted in a branch of its own), 64 57, 256 95, 400 101.
+// stores decide beside the memory: those of a row's alternatives, 4 bytes at a time, made it 21.6.  Channel-major, 168 MB of scores, 0, 3 and
+// 20 alternatives: fp32, 16 classes 31 us, 43 and -, 64 36, 43 and 136, 256 54, 111 and 429, 400 60, 244 and 1316; bf16, 16 classes 37, 73 and - (113
+// when each load was converted in a branch of its own), 64 48, 78 and 259, 256 94, 203 and 814, 400 93, 382 and 2098.  (R = 0 reads all scores
+// twice and once more for each alternative.)
 template <class T, int W, int R, bool ROWS>
 __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void logp_lanes_kernel(const T *__restrict__ x, LogpArgs a)
 {
@@ -860,8 +862,8 @@ __device__ __forceinline__ void logp_bwd_far_row(const T *at, T *to, int C, Logp
 }
 
 // Point-major: L lanes to a row, U times 16 bytes each, `chunks` workgroups behind one another along long rows (L = 256).  Bound by memory
-// where rows fill their lanes: 336 MB of scores and as much of gradients, bf16, 64 classes 126 us (5.3 TB/s), 100 classes 210, 600 117, 131072
-// 112 (6.0 TB/s); fp32, 40 classes 164, 512 114, 131072 118.
+// where rows fill their lanes: 336 MB of scores and as much of gradients, bf16, 64 classes 125 us (5.3 TB/s), 100 classes 221, 600 116, 131072
+// 112 (6.0 TB/s); fp32, 40 classes 146, 600 116, 131072 113; with scores about 200: bf16 200, 300, 167 and 234, fp32 242, 149 and 263.
 template <class T, int L, int U>
 __global__ __launch_bounds__(256) void logp_bwd_rows_kernel(const T *x, T *gx, LogpBwdArgs a, int chunks)
 {
@@ -927,7 +929,8 @@ __global__ __launch_bounds__(256) void logp_bwd_few_kernel(const T *x, T *gx, Lo
 }
 
 // Channel-major: a lane to a position, a workgroup to 256 of them and 16 classes.  168 MB of scores and as much of gradients: fp32,
-// 16 classes 84 us, 64 78, 256 74; bf16, which a wave loads in half lines, 16 classes 110, 64 104, 256 94.
+// 16 classes 81 us, 64 76, 256 74; bf16, which a wave loads in half lines, 16 classes 110, 64 108, 256 95; with scores about 200, fp32 102, 214 and
+// 181, bf16 142, 351 and 260.
 constexpr int BWD_CLASSES = 16;
 template <class T>
 __global__ __launch_bounds__(256) void logp_bwd_cols_kernel(const T *x, T *gx, LogpBwdArgs a, unsigned tiles, unsigned parts)

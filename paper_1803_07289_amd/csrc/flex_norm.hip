@@ -166,7 +166,8 @@ __global__ __launch_bounds__(L > 256 ? L : 256) void norm_rows_kernel(const T *_
         }
 }
 
-// Rows of any length, a workgroup to each, read three times.
+// Rows of any length, a workgroup to each, read three times, an element to a lane.  x of 168 MB, forward and backward: 20000 channels fp32 137
+// and 226 us, bf16 233 and 419; 2^20 channels, which leave most compute units without a row, fp32 1212 and 1268, bf16 1510 and 2012.
 template <class T>
 __global__ __launch_bounds__(1024) void norm_long_rows_kernel(const T *__restrict__ x, Param<T> w, Param<T> b, T *__restrict__ y,
                                                               float *mean_out, float *rstd_out, int C, float eps)
@@ -424,7 +425,7 @@ __global__ __launch_bounds__(rows_bwd_threads(L)) void norm_rows_bwd_kernel(cons
 // at least two.  A wave's vector operations decide beside the memory, 14 an element: nothing in a turn is chosen by a lane's place, what
 // is another lane's has weight 0 in the row's sums and is left out when the parameters' are stored.
 // 8188 x 5120 bf16: 46 us with the 4 us of the partial sums' sum (5.5 TB/s; adding x and grad_out 44), without the parameters' 42.
-// x, grad_out and grad_x of 504 MB: bf16, 264 channels 102 to 136 us (33 of 64 lanes), 512 98, 1000 100, 2048
+// x, grad_out and grad_x of 504 MB: bf16, 264 channels 101 us (33 of 64 lanes), 512 98, 1000 100, 2048
 // 97, 8192 101; fp32, 132 channels 96, 1024 95, 4096 97.
 template <class T, bool PARAMS, bool GRAD_X, int D>
 __global__ __launch_bounds__(1024) void norm_wide_rows_bwd_kernel(const T *__restrict__ x, Param<T> w, const T *__restrict__ g,
@@ -583,8 +584,8 @@ __global__ __launch_bounds__(256) void norm_long_rows_params_kernel(const T *__r
 // ---- channel-major ----------------------------------------------------------------------------------------------------------
 // A lane to P positions, W waves of a workgroup share the channels: R of them a wave in registers, or (R = 0) any number, read again.
 // P = 2 of 16 bits, so that a wave's loads are whole lines.
-// Bound by memory.  us, x of 168 MB, forward and backward: fp32, 16 channels 81 and 133, 64 83 and 140, 200 81 and 116, 400 130 and 243; bf16,
-// 16 channels 88 and 137 (a position to a lane 105 and 158), 64 87 and 143 (113 and 171), 200 91 and 149 (115 and 149), 400 158 and 320.
+// Bound by memory.  us, x of 168 MB, forward and backward: fp32, 16 channels 81 and 133, 64 83 and 140, 200 81 and 116, 400 124 and 243; bf16,
+// 16 channels 88 and 137 (a position to a lane 105 and 158), 64 87 and 143 (113 and 171), 200 91 and 149 (115 and 149), 400 222 and 414.
 constexpr int COL_CHANNELS = 16;
 
 // sums over the waves of a workgroup, by position
