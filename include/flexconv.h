@@ -448,6 +448,8 @@ int flexnorm_bwd(const void *x, const void *weight, const void *grad_out, const 
  * A score of -inf is a masked class: no share, never an alternative; where fewer classes are left than asked for, the others are
  * (-inf, -1).  A position with nothing but -inf has lse = logp = -inf, entropy 0.  NaN or +inf among the scores: logp, entropy and
  * lse are NaN, NaN is never an alternative.
+ * All but lse (one fp32 number, rounded) come from differences to the position's largest score: scores of any size have the same
+ * precision.  No log probability is above 0, no entropy below.
  * row_stride (elements): point-major from one position's scores to the next one's, at least C (rows of a padded vocabulary);
  * channel-major from one class's scores to the next one's, at least N.  C <= FLEX_LOGP_MAX_CLASSES.
  * Long rows that are few are cut in parts, which meet in the workspace; FLEX_LOGP_NO_WORKSPACE bytes: not so, workspace may be NULL.
@@ -490,7 +492,7 @@ int flexlogp_bwd(const void *logits, const int32_t *target, const float *lse, co
  * flexadamw_step: grads host array of n device pointers, all of grad_dtype, in memory that none of the list's tensors is in; NULL: that
  * tensor is left as it is.  lr, or *lr_dev
  * where lr_dev (device) is not NULL; grad_scale device, or NULL for 1.  A grad_scale that is not finite: nothing is changed and
- * the step is not counted (a loss scale that overflowed, decided on the device).  Gradients must be finite otherwise.
+ * the step is not counted (a loss scale that overflowed, decided on the device).  Gradients must be finite otherwise, and so must their squares.
  */
 #define FLEX_ADAMW_STEPS_AT 32
 typedef struct {
