@@ -862,8 +862,8 @@ __device__ __forceinline__ void logp_bwd_far_row(const T *at, T *to, int C, Logp
 }
 
 // Point-major: L lanes to a row, U times 16 bytes each, `chunks` workgroups behind one another along long rows (L = 256).  Bound by memory
-// where rows fill their lanes: 336 MB of scores and as much of gradients, bf16, 64 classes 125 us (5.3 TB/s), 100 classes 221, 600 116, 131072
-// 112 (6.0 TB/s); fp32, 40 classes 146, 600 116, 131072 113; with scores about 200: bf16 200, 300, 167 and 234, fp32 242, 149 and 263.
+// where rows fill their lanes: 336 MB of scores and as much of gradients, bf16, 64 classes 125 us (5.3 TB/s), 100 classes 218, 600 115, 131072
+// 112 (6.0 TB/s); fp32, 40 classes 145, 600 115, 131072 112; with scores about 200: bf16 199, 293, 166 and 234, fp32 242, 148 and 263.
 template <class T, int L, int U>
 __global__ __launch_bounds__(256) void logp_bwd_rows_kernel(const T *x, T *gx, LogpBwdArgs a, int chunks)
 {
@@ -874,20 +874,24 @@ __global__ __launch_bounds__(256) void logp_bwd_rows_kernel(const T *x, T *gx, L
     T *to = gx + row * a.grad_stride;
     const int c0 = ((L == 256 ? (int)(blockIdx.x % chunks) * U * L : 0) + (int)(threadIdx.x % L)) * N;
     const LogpBwdRow f(a, row);
-    float v[U][N];
-    // (in place no lane may read what another one writes: the row's end is read element by element, after all else has been asked for)
+    // (in place no lane may read what another one writes: the elements of the row's end, fewer than a piece, are their lane's own; of
+    // several pieces they have registers and operations of their own, so that no other piece waits for them: bf16, 1500 classes 134 and 128 us; of
+    // one piece they share its operations: bf16, 100 classes 218 and, apart, 243)
+    constexpr bool APART = U > 1;
     typename Chunk<T>::V raw[U];
+    T last[N - 1];
+    const int end = a.C / N * N;
+    const bool has_end = end < a.C && end >= c0 && end < c0 + U * L * N && (end - c0) % (L * N) == 0;
 #pragma unroll
     for (int u = 0; u < U; ++u)
         if (!f.zero && c0 + u * L * N + N <= a.C) raw[u] = *(const typename Chunk<T>::V *)(at + c0 + u * L * N);
+    if (!f.zero && has_end)
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-        const int c = c0 + u * L * N;
-        if (!f.zero && c < a.C && c + N > a.C)
-#pragma unroll
-            for (int j = 0; j < N; ++j)
-                if (c + j < a.C) raw[u][j] = at[c + j];
-    }
+        for (int j = 0; j < N - 1; ++j)
+            if (end + j < a.C) {
+                if (APART) last[j] = at[end + j];
+                else raw[0][j] = at[end + j];
+            }
     if (__builtin_expect(f.far(), 0)) {
         if (L < 256 || blockIdx.x % chunks == row % chunks) logp_bwd_far_row<T, L>(at, to, a.C, f);        // (all the XCDs have some)
         return;
@@ -895,10 +899,17 @@ __global__ __launch_bounds__(256) void logp_bwd_rows_kernel(const T *x, T *gx, L
 #pragma unroll
     for (int u = 0; u < U; ++u) {
         const int c = c0 + u * L * N;
+        if (APART && c + N > a.C) break;
+        float v[N];
 #pragma unroll
-        for (int j = 0; j < N; ++j) v[u][j] = f.zero ? 0.f : f(to_f32(raw[u][j]), c + j);
-        Chunk<T>::store_row(to, c, a.C, v[u]);
+        for (int j = 0; j < N; ++j) v[j] = f.zero ? 0.f : f(to_f32(raw[u][j]), c + j);
+        if (APART) Chunk<T>::store(to + c, v);
+        else Chunk<T>::store_row(to, c, a.C, v);
     }
+    if (APART && has_end)
+#pragma unroll
+        for (int j = 0; j < N - 1; ++j)
+            if (end + j < a.C) to[end + j] = (T)(f.zero ? 0.f : f(to_f32(last[j]), end + j));
 }
 
 // Point-major rows of up to R classes, one to a lane.
